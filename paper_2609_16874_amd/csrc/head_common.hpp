@@ -1,0 +1,75 @@
+// head_common.hpp -- element types, vector access and activations shared by
+// the head operators (group norm, linear).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "cpe_head.h"
+
+namespace cpe {
+
+typedef __bf16 bf16_t;
+
+// V elements that need no more than their own alignment: global memory
+// serves vector accesses at any element boundary with the same instruction.
+template <typename T, int V>
+struct __attribute__((packed, aligned(sizeof(T)))) Vec {
+    T v[V];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load_vec(const T *p)
+{
+    return *reinterpret_cast<const Vec<T, V> *>(p);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const Vec<T, V> &v)
+{
+    *reinterpret_cast<Vec<T, V> *>(p) = v;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float sigmoid(float u)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * u));
+}
+
+// Standard normal distribution function Phi(u) = (1 + erf(u / sqrt 2)) / 2.
+__device__ __forceinline__ float normal_cdf(float u) { return 0.5f * (1.0f + erff(0.70710678118654752f * u)); }
+
+// act(u), in binary32.  A NaN stays a NaN; SiLU and GELU of -infinity are
+// the product -inf * 0, a NaN.
+template <int ACT>
+__device__ __forceinline__ float activate(float u)
+{
+    if constexpr (ACT == CPE_ACT_RELU) return u < 0.0f ? 0.0f : u;
+    if constexpr (ACT == CPE_ACT_SILU) return u * sigmoid(u);
+    if constexpr (ACT == CPE_ACT_GELU) return u * normal_cdf(u);
+    return u;
+}
+
+// act'(u); ReLU's derivative at 0 is 0.
+template <int ACT>
+__device__ __forceinline__ float activate_grad(float u)
+{
+    if constexpr (ACT == CPE_ACT_RELU) return u > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == CPE_ACT_SILU) {
+        const float s = sigmoid(u);
+        return s * (1.0f + u * (1.0f - s));
+    }
+    if constexpr (ACT == CPE_ACT_GELU)
+        return normal_cdf(u) + u * 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * u * u);
+    return 1.0f;
+}
+
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+inline size_t element_size(cpe_dtype t) { return t == CPE_F32 ? 4 : 2; }
+inline size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace cpe

@@ -1,0 +1,55 @@
+// linear.hpp -- arguments of the matrix product kernels (private to the library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cpe_head.h"
+
+namespace cpe {
+
+constexpr int kGemmThreads = 256;
+constexpr int kTile = 128;                    // output rows and columns of a workgroup
+constexpr int kSplitTiles = 512;              // partial tiles of a split product (its scratch)
+constexpr int64_t kMaxTiles = (int64_t)1 << 22;
+constexpr int kSumBlocks = 1024;              // workgroups along the rows of the bias gradient
+
+// out[m][n] = act(sum_k A(m, k) B(n, k) + bias[n]) + residual[m][n].
+// A(m, k) is a[m lda + k], or a[k lda + m] where a_cols is set; B alike.
+struct GemmArgs {
+    const void *a, *b;
+    int64_t lda, ldb;
+    int32_t m, n, k;
+    bool a_cols, b_cols;
+    void *out;
+    int64_t ldo;
+    const float *bias;                        // may be null
+    const void *residual;                     // may be null
+    int64_t ldr;
+    void *preact;                             // may be null: the value before the activation
+    int64_t ldp;
+    int act;
+    float *part;                              // scratch of a split product: [splits][m][n rounded up to 4]
+    int32_t splits, k_split;                  // splits > 1: each sums k_split of the k
+    int32_t tiles_m, tiles_n;
+};
+
+// dz = dy act'(preact) (dz may be null) and column sums of it (sums may be null).
+struct GradArgs {
+    const void *dy, *preact;
+    int64_t ldd, ldp, ldz;
+    void *dz;
+    float *part, *sums;                       // scratch [blocks][n]; out [n]
+    int32_t rows, n, blocks;
+    int act;
+};
+
+hipError_t launch_gemm_f32(const GemmArgs &g, hipStream_t stream);
+hipError_t launch_gemm_f16(const GemmArgs &g, hipStream_t stream);
+hipError_t launch_gemm_bf16(const GemmArgs &g, hipStream_t stream);
+hipError_t launch_grad_f32(const GradArgs &g, hipStream_t stream);
+hipError_t launch_grad_f16(const GradArgs &g, hipStream_t stream);
+hipError_t launch_grad_bf16(const GradArgs &g, hipStream_t stream);
+
+}  // namespace cpe

@@ -1,0 +1,36 @@
+// norm.hpp -- arguments of the group norm kernels (private to the library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cpe_head.h"
+
+namespace cpe {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormBlocks = 2048;      // workgroups of a pass over the map (or one per sample)
+constexpr int kNormMaxChannels = 8192;
+
+struct NormArgs {
+    const void *x, *dy;
+    void *out;                          // y or dx (dx may be null)
+    int64_t x_ld, x_sample, dy_ld, dy_sample, out_ld, out_sample;
+    const float *gamma, *beta;          // may be null
+    const int32_t *valid;               // may be null
+    float *stats;                       // [samples][G][2]: written by the forward, read by the backward
+    float *part;                        // scratch: [samples][blocks][G or C][2]
+    float *chan;                        // scratch: [samples][C][2] (backward)
+    float *dgamma, *dbeta;              // may be null
+    int32_t samples, pixels, channels, groups, blocks;
+    float eps;
+    int act;
+    bool backward;
+};
+
+hipError_t launch_norm_f32(const NormArgs &a, hipStream_t stream);
+hipError_t launch_norm_f16(const NormArgs &a, hipStream_t stream);
+hipError_t launch_norm_bf16(const NormArgs &a, hipStream_t stream);
+
+}  // namespace cpe

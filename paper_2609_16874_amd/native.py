@@ -18,18 +18,21 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcpe_decode.so")
 
 CPE_OK, CPE_ERR_INVALID_ARG, CPE_ERR_UNSUPPORTED, CPE_ERR_OUT_OF_MEMORY, CPE_ERR_HIP = range(5)
-CPE_F32, CPE_F16 = 0, 1
+CPE_F32, CPE_F16, CPE_BF16 = 0, 1, 2
 W_KEYS = 8192
 
 CENTROID_DTYPE = np.dtype([("bin_x", "<i4"), ("bin_y", "<i4"), ("x", "<f4"), ("y", "<f4"),
                            ("score", "<f8"), ("npix", "<i4"), ("reserved", "<i4")])
 
-# Every entry point declared in include/cpe_decode.h.
+# Every entry point declared in include/cpe_decode.h and include/cpe_head.h.
 EXPORTS = ("cpe_decode_create", "cpe_decode", "cpe_decode_ex", "cpe_decode_masks", "cpe_decode_destroy",
            "cpe_status_string", "cpe_decode_get_tables", "cpe_decode_get_histogram", "cpe_decode_workspace_bytes",
            "cpe_decode_set_stage_events", "cpe_decode_naive", "cpe_check_sqrt",
            "cpe_decode_test_fail_launch", "cpe_decode_noalloc", "cpe_decode_launch_count",
-           "cpe_decode_test_search_mode", "cpe_decode_test_separate_list")
+           "cpe_decode_test_search_mode", "cpe_decode_test_separate_list",
+           "cpe_norm_create", "cpe_norm_forward", "cpe_norm_backward", "cpe_norm_destroy",
+           "cpe_norm_workspace_bytes", "cpe_linear_create", "cpe_linear_forward", "cpe_linear_backward",
+           "cpe_linear_destroy", "cpe_linear_workspace_bytes")
 STAGE_EVENTS = 6
 MFMA_BINS = 32
 
@@ -100,6 +103,27 @@ def library():
         lib.cpe_decode_test_separate_list.argtypes = [P, i32]
         lib.cpe_check_sqrt.restype = i32
         lib.cpe_check_sqrt.argtypes = [P, P]
+        i64 = ctypes.c_int64
+        lib.cpe_norm_create.restype = i32
+        lib.cpe_norm_create.argtypes = [ctypes.POINTER(P), i32, i32, i32, i32, i32, i32, ctypes.c_float]
+        lib.cpe_norm_forward.restype = i32
+        lib.cpe_norm_forward.argtypes = [P, P, i32, i32, P, i64, i64, P, P, P, P, i64, i64, P]
+        lib.cpe_norm_backward.restype = i32
+        lib.cpe_norm_backward.argtypes = [P, P, i32, i32, P, i64, i64, P, i64, i64, P, P, P, P, P, i64, i64, P, P]
+        lib.cpe_norm_destroy.restype = i32
+        lib.cpe_norm_destroy.argtypes = [P]
+        lib.cpe_norm_workspace_bytes.restype = ctypes.c_size_t
+        lib.cpe_norm_workspace_bytes.argtypes = [P]
+        lib.cpe_linear_create.restype = i32
+        lib.cpe_linear_create.argtypes = [ctypes.POINTER(P), i32, i32, i32, i32, i32]
+        lib.cpe_linear_forward.restype = i32
+        lib.cpe_linear_forward.argtypes = [P, P, i32, P, i64, P, i64, P, P, i64, P, i64, P, i64]
+        lib.cpe_linear_backward.restype = i32
+        lib.cpe_linear_backward.argtypes = [P, P, i32, P, i64, P, i64, P, i64, P, i64, P, i64, P, i64, P]
+        lib.cpe_linear_destroy.restype = i32
+        lib.cpe_linear_destroy.argtypes = [P]
+        lib.cpe_linear_workspace_bytes.restype = ctypes.c_size_t
+        lib.cpe_linear_workspace_bytes.argtypes = [P]
         _lib = lib
     return _lib
 
@@ -283,4 +307,4 @@ def check_sqrt(stream=None) -> int:
 
 def torch_dtype(dtype: str):
     import torch
-    return {"f32": torch.float32, "f16": torch.float16}[dtype]
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
