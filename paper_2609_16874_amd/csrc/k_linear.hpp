@@ -293,19 +293,32 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs g)
     }
 }
 
-// The splits' partial products summed in order, then the epilogue.
+// The splits' partial products summed in a fixed order, then the epilogue:
+// 16 vectors of four n per workgroup, 16 lanes of splits for each.
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g)
 {
-    const int quads = (g.n + 3) / 4;
-    const int64_t all = (int64_t)g.m * quads, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= all) return;
-    const int m = (int)(at / quads), n = (int)(at - (int64_t)m * quads) * 4;
-    const float *p = g.part + (int64_t)m * quads * 4 + n;
-    const int64_t step = (int64_t)g.m * quads * 4;
-    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
-    for (int s = 1; s < g.splits; s++) v += *reinterpret_cast<const f32x4 *>(p + s * step);
-    finish<ACT, T>(g, m, n, v);
+    __shared__ f32x4 lds[4][16];
+    const int quads = (g.n + 3) / 4, at = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    const int64_t all = (int64_t)g.m * quads, q = (int64_t)blockIdx.x * 16 + at;
+    const int64_t step = all * 4;
+    const float *p = g.part + q * 4;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (q < all) {
+#pragma unroll 4
+        for (int s = lane; s < g.splits; s += 16) v += *reinterpret_cast<const f32x4 *>(p + s * step);
+    }
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] += __shfl_xor(v[i], o);
+    if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][at] = v;
+    __syncthreads();
+    if (threadIdx.x < 16 && q < all) {
+        v = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
+        const int m = (int)(q / quads);
+        finish<ACT, T>(g, m, (int)(q - (int64_t)m * quads) * 4, v);
+    }
 }
 
 // Few rows (a served token or a handful): 16 n per workgroup, its waves
@@ -409,18 +422,25 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
     }
 }
 
-// sums[n] over the workgroups' partials: 64 columns per workgroup.
-__global__ __launch_bounds__(256) void k_column_join(GradArgs g)
+// sums[n] over the workgroups' partials: 32 columns (a cache line) per
+// workgroup, 32 lanes of partials each.
+__global__ __launch_bounds__(1024) void k_column_join(GradArgs g)
 {
-    __shared__ double lds[256];
-    const int n = blockIdx.x * 64 + (threadIdx.x & 63);
+    __shared__ double lds[16][32];
+    const int at = threadIdx.x & 31, n = blockIdx.x * 32 + at;
     double s = 0.0;
-    if (n < g.n)
-        for (int i = threadIdx.x >> 6; i < g.blocks; i += 4) s += (double)g.part[(int64_t)i * g.n + n];
-    lds[threadIdx.x] = s;
+    if (n < g.n) {
+#pragma unroll 8
+        for (int i = threadIdx.x >> 5; i < g.blocks; i += 32) s += (double)g.part[(int64_t)i * g.n + n];
+    }
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 63) < 32) lds[threadIdx.x >> 6][at] = s;
     __syncthreads();
-    if (threadIdx.x < 64 && n < g.n)
-        g.sums[n] = (float)(s + lds[threadIdx.x + 64] + lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
+    if (threadIdx.x < 32 && n < g.n) {
+        s = 0.0;
+        for (int w = 0; w < 16; w++) s += lds[w][at];
+        g.sums[n] = (float)s;
+    }
 }
 
 // -- launches -----------------------------------------------------------------------
@@ -465,7 +485,7 @@ hipError_t launch_tiles(GemmArgs g, hipStream_t stream)
         hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, false, ACT>), grid, dim3(kGemmThreads), 0, stream, g);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || g.splits == 1) return e;
     const int64_t quads = (int64_t)g.m * ((g.n + 3) / 4);
-    hipLaunchKernelGGL((k_gemm_join<T, ACT>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((k_gemm_join<T, ACT>), dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, stream, g);
     return hipGetLastError();
 }
 
@@ -535,7 +555,7 @@ hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
     default: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_NONE>), grid, dim3(256), 0, stream, g); break;
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !g.sums) return e;
-    hipLaunchKernelGGL(k_column_join, dim3((unsigned)ceil_div(g.n, 64)), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL(k_column_join, dim3((unsigned)ceil_div(g.n, 32)), dim3(1024), 0, stream, g);
     return hipGetLastError();
 }
 

@@ -46,6 +46,50 @@ __device__ __forceinline__ RowRange row_range(const NormArgs &a)
     return r;
 }
 
+// c / cpg for c < 8192 through the reciprocal: c + 1/2 is at least 1/2 from a
+// multiple of cpg, and the product's error stays under 1e-3 / cpg.
+__device__ __forceinline__ int group_of(int c, float inv_cpg) { return (int)(((float)c + 0.5f) * inv_cpg); }
+
+// A vector's channels: their groups' statistics, and gamma and beta.
+template <int V>
+struct Channels {
+    float mean[V], rstd[V], gamma[V], beta[V];
+    __device__ __forceinline__ Channels(const NormArgs &a, int b, int col)
+    {
+        const int cpg = a.channels / a.groups;
+        const float inv_cpg = 1.0f / (float)cpg;
+        const float2 *stats = reinterpret_cast<const float2 *>(a.stats) + (int64_t)b * a.groups;
+        if (cpg % V == 0) {         // all in one group
+            const float2 st = stats[group_of(col * V, inv_cpg)];
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                mean[v] = st.x;
+                rstd[v] = st.y;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                const float2 st = stats[group_of(col * V + v, inv_cpg)];
+                mean[v] = st.x;
+                rstd[v] = st.y;
+            }
+        }
+        Vec<float, V> g, s;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            g.v[v] = 1.0f;
+            s.v[v] = 0.0f;
+        }
+        if (a.gamma) g = load_vec<float, V>(a.gamma + col * V);
+        if (a.beta) s = load_vec<float, V>(a.beta + col * V);
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            gamma[v] = g.v[v];
+            beta[v] = s.v[v];
+        }
+    }
+};
+
 // How a workgroup covers a row of C channels.
 template <int V>
 struct Columns {
@@ -155,33 +199,53 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
     }
 }
 
-// stats[b][g] = (mean, rstd) from the workgroups' partials, one wave each.
-template <typename T>
-__global__ __launch_bounds__(64) void k_norm_merge(NormArgs a)
+// stats[b][g] = (mean, rstd) from the workgroups' partials: one workgroup per
+// group, its threads' at most kMergeEach partials in flight together.
+constexpr int kMergeEach = 8;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_merge(NormArgs a)
 {
+    __shared__ double lds[2][THREADS / 64];
     const int b = blockIdx.x / a.groups, g = blockIdx.x - b * a.groups;
     const int pb = valid_pixels(a, b), cpg = a.channels / a.groups;
     const int64_t step = rows_per_block(pb, a.blocks);
     const float2 *part = reinterpret_cast<const float2 *>(a.part) + (int64_t)b * a.blocks * a.groups + g;
-    auto rows = [&](int i) {
+    float2 p[kMergeEach];
+    double rows[kMergeEach];
+#pragma unroll
+    for (int e = 0; e < kMergeEach; e++) {
+        const int i = threadIdx.x + e * THREADS;
         const int64_t left = pb - step * i;
-        return (double)(left < 0 ? 0 : left < step ? left : step);
+        const bool on = i < a.blocks && left > 0;
+        p[e] = on ? part[(int64_t)i * a.groups] : make_float2(0.0f, 0.0f);
+        rows[e] = (double)(!on ? 0 : left < step ? left : step);
+    }
+    auto total = [&](double v, int slot) {
+        v = sum_lanes(v, 64);
+        if constexpr (THREADS == 64) return v;
+        if ((threadIdx.x & 63) == 0) lds[slot][threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0;
+        for (int w = 0; w < THREADS / 64; w++) v += lds[slot][w];
+        return v;
     };
     const double n = pb > 0 ? pb : 1;
     double mean = 0.0, m2 = 0.0;
-    for (int i = threadIdx.x; i < a.blocks; i += 64) mean += rows(i) * (double)part[(int64_t)i * a.groups].x;
-    mean = sum_lanes(mean, 64) / n;
-    for (int i = threadIdx.x; i < a.blocks; i += 64) {
-        const float2 p = part[(int64_t)i * a.groups];
-        const double d = (double)p.x - mean, r = rows(i);
-        if (r > 0.0) m2 += (double)p.y + r * cpg * d * d;
+#pragma unroll
+    for (int e = 0; e < kMergeEach; e++) mean += rows[e] * (double)p[e].x;
+    mean = total(mean, 0) / n;
+#pragma unroll
+    for (int e = 0; e < kMergeEach; e++) {
+        const double d = (double)p[e].x - mean;
+        if (rows[e] > 0.0) m2 += (double)p[e].y + rows[e] * cpg * d * d;
     }
-    m2 = sum_lanes(m2, 64);
+    m2 = total(m2, 1);
     if (threadIdx.x == 0) {
         const double var = m2 > 0.0 || m2 != m2 ? m2 / (n * cpg) : 0.0;
         reinterpret_cast<float2 *>(a.stats)[blockIdx.x] = make_float2((float)mean, (float)(1.0 / sqrt(var + a.eps)));
     }
 }
+static_assert(kNormBlocks <= 256 * kMergeEach, "every partial of a group has a place");
 
 // y = act((x - mean) (rstd gamma) + beta); pixels from the sample's count on
 // are set to 0.
@@ -190,26 +254,21 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 {
     const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
     const Columns<V> cols(a.channels);
-    const int pb = valid_pixels(a, b), cpg = a.channels / a.groups;
+    const int pb = valid_pixels(a, b);
     const int64_t span = rows_per_block(a.pixels, a.blocks), lo = span * i;
     const int64_t hi = lo + span < a.pixels ? lo + span : a.pixels;
     const T *x = static_cast<const T *>(a.x) + b * a.x_sample;
     T *y = static_cast<T *>(a.out) + b * a.out_sample;
-    const float2 *stats = reinterpret_cast<const float2 *>(a.stats) + (int64_t)b * a.groups;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        float mean[V], scale[V], shift[V];
+        const Channels<V> ch(a, b, col);
+        float scale[V];
 #pragma unroll
-        for (int v = 0; v < V; v++) {
-            const int c = col * V + v;
-            const float2 st = stats[c / cpg];
-            mean[v] = st.x;
-            scale[v] = a.gamma ? st.y * a.gamma[c] : st.y;
-            shift[v] = a.beta ? a.beta[c] : 0.0f;
-        }
+        for (int v = 0; v < V; v++) scale[v] = ch.rstd[v] * ch.gamma[v];
         auto one = [&](const Vec<T, V> &f) {
             Vec<T, V> o;
 #pragma unroll
-            for (int v = 0; v < V; v++) o.v[v] = (T)activate<ACT>(fmaf((float)f.v[v] - mean[v], scale[v], shift[v]));
+            for (int v = 0; v < V; v++)
+                o.v[v] = (T)activate<ACT>(fmaf((float)f.v[v] - ch.mean[v], scale[v], ch.beta[v]));
             return o;
         };
         const int64_t xs = cols.rows * a.x_ld, ys = cols.rows * a.out_ld;
@@ -234,26 +293,6 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
     }
 }
 
-// Channel constants of the gradient: xh = (x - mean) rstd, u = xh gamma + beta.
-template <int V>
-struct GradChannels {
-    float mean[V], rstd[V], gamma[V], beta[V];
-    __device__ __forceinline__ GradChannels(const NormArgs &a, int b, int col)
-    {
-        const int cpg = a.channels / a.groups;
-        const float2 *stats = reinterpret_cast<const float2 *>(a.stats) + (int64_t)b * a.groups;
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            const int c = col * V + v;
-            const float2 st = stats[c / cpg];
-            mean[v] = st.x;
-            rstd[v] = st.y;
-            gamma[v] = a.gamma ? a.gamma[c] : 1.0f;
-            beta[v] = a.beta ? a.beta[c] : 0.0f;
-        }
-    }
-};
-
 // part[b][block][c] = (sum du, sum du xh) over the block's rows.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
@@ -264,7 +303,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
     const int C = a.channels, n_rows = rr.r1 - rr.r0;
     float *l1 = lds, *l2 = lds + cols.rows * C;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const GradChannels<V> ch(a, rr.b, col);
+        const Channels<V> ch(a, rr.b, col);
+        float scale[V];
+#pragma unroll
+        for (int v = 0; v < V; v++) scale[v] = ch.rstd[v] * ch.gamma[v];
         const int64_t first = rr.r0 + cols.row;
         const T *px = static_cast<const T *>(a.x) + rr.b * a.x_sample + col * V + first * a.x_ld;
         const T *pd = static_cast<const T *>(a.dy) + rr.b * a.dy_sample + col * V + first * a.dy_ld;
@@ -276,10 +318,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
         auto add = [&](const Vec<T, V> &fx, const Vec<T, V> &fd) {
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                const float xh = ((float)fx.v[v] - ch.mean[v]) * ch.rstd[v];
-                const float du = (float)fd.v[v] * activate_grad<ACT>(fmaf(xh, ch.gamma[v], ch.beta[v]));
+                const float d = (float)fx.v[v] - ch.mean[v];
+                const float du = (float)fd.v[v] * activate_grad<ACT>(fmaf(d, scale[v], ch.beta[v]));
                 s1[v] += du;
-                s2[v] = fmaf(du, xh, s2[v]);
+                s2[v] = fmaf(du, d, s2[v]);
             }
         };
         for (; n >= kNormUnroll; n -= kNormUnroll) {
@@ -299,7 +341,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
         for (int v = 0; v < V; v++) {
             const int at = cols.row * C + col * V + v;
             l1[at] = s1[v];
-            l2[at] = s2[v];
+            l2[at] = s2[v] * ch.rstd[v];
         }
     }
     __syncthreads();
@@ -314,29 +356,39 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
     }
 }
 
-// chan[b][c] = the workgroups' partials summed: 64 channels of a sample per
-// workgroup, its four waves each a quarter of the partials.
-template <typename T>
-__global__ __launch_bounds__(kNormThreads) void k_norm_grad_merge(NormArgs a)
+// chan[b][c] = the workgroups' partials summed: kMergeChannels channels of a
+// sample (a cache line of partials) per workgroup, 64 lanes of partials each.
+constexpr int kMergeChannels = 16, kMergeLanes = 64;
+__global__ __launch_bounds__(kMergeChannels *kMergeLanes) void k_norm_grad_merge(NormArgs a)
 {
-    __shared__ double l1[kNormThreads], l2[kNormThreads];
-    const int slabs = (a.channels + 63) / 64;
-    const int b = blockIdx.x / slabs, c = (blockIdx.x - b * slabs) * 64 + (threadIdx.x & 63);
+    __shared__ double l1[kMergeLanes / 4][kMergeChannels], l2[kMergeLanes / 4][kMergeChannels];
+    const int slabs = (a.channels + kMergeChannels - 1) / kMergeChannels;
+    const int b = blockIdx.x / slabs, at = threadIdx.x % kMergeChannels, lane = threadIdx.x / kMergeChannels;
+    const int c = (blockIdx.x - b * slabs) * kMergeChannels + at;
     const float2 *part = reinterpret_cast<const float2 *>(a.part) + (int64_t)b * a.blocks * a.channels;
     double s1 = 0.0, s2 = 0.0;
-    if (c < a.channels)
-        for (int i = threadIdx.x >> 6; i < a.blocks; i += kNormThreads / 64) {
+    if (c < a.channels) {
+#pragma unroll 8
+        for (int i = lane; i < a.blocks; i += kMergeLanes) {
             const float2 p = part[(int64_t)i * a.channels + c];
             s1 += (double)p.x;
             s2 += (double)p.y;
         }
-    l1[threadIdx.x] = s1;
-    l2[threadIdx.x] = s2;
+    }
+    // a wave holds four lanes of partials, sixteen threads apart
+    s1 += __shfl_xor(s1, 16);
+    s2 += __shfl_xor(s2, 16);
+    s1 += __shfl_xor(s1, 32);
+    s2 += __shfl_xor(s2, 32);
+    if ((threadIdx.x & 63) < kMergeChannels) {
+        l1[threadIdx.x >> 6][at] = s1;
+        l2[threadIdx.x >> 6][at] = s2;
+    }
     __syncthreads();
-    if (threadIdx.x < 64 && c < a.channels) {
-        for (int w = 1; w < kNormThreads / 64; w++) {
-            s1 += l1[threadIdx.x + 64 * w];
-            s2 += l2[threadIdx.x + 64 * w];
+    if (threadIdx.x < kMergeChannels && c < a.channels) {
+        for (int w = 1; w < kMergeLanes / 4; w++) {
+            s1 += l1[w][at];
+            s2 += l2[w][at];
         }
         reinterpret_cast<float2 *>(a.chan)[(int64_t)b * a.channels + c] = make_float2((float)s1, (float)s2);
     }
@@ -387,22 +439,25 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a)
     const int64_t span = rows_per_block(a.pixels, a.blocks), lo = span * i;
     const int64_t hi = lo + span < a.pixels ? lo + span : a.pixels;
     const int64_t end = hi < pb ? hi : pb;
+    const float inv_cpg = 1.0f / (float)cpg;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const GradChannels<V> ch(a, b, col);
-        float ga[V], gq[V];
+        // dx = du (rstd gamma) - rstd a/n - (x - mean) rstd^2 q/n
+        const Channels<V> ch(a, b, col);
+        float scale[V], flat[V], slope[V];
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            const int g = (col * V + v) / cpg;
-            ga[v] = lds[2 * g];
-            gq[v] = lds[2 * g + 1];
+            const int g = group_of(col * V + v, inv_cpg);
+            scale[v] = ch.rstd[v] * ch.gamma[v];
+            flat[v] = -ch.rstd[v] * lds[2 * g];
+            slope[v] = -ch.rstd[v] * ch.rstd[v] * lds[2 * g + 1];
         }
         auto one = [&](const Vec<T, V> &fx, const Vec<T, V> &fd) {
             Vec<T, V> o;
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                const float xh = ((float)fx.v[v] - ch.mean[v]) * ch.rstd[v];
-                const float du = (float)fd.v[v] * activate_grad<ACT>(fmaf(xh, ch.gamma[v], ch.beta[v]));
-                o.v[v] = (T)(ch.rstd[v] * (fmaf(du, ch.gamma[v], -ga[v]) - xh * gq[v]));
+                const float d = (float)fx.v[v] - ch.mean[v];
+                const float du = (float)fd.v[v] * activate_grad<ACT>(fmaf(d, scale[v], ch.beta[v]));
+                o.v[v] = (T)fmaf(du, scale[v], fmaf(d, slope[v], flat[v]));
             }
             return o;
         };
@@ -453,7 +508,10 @@ hipError_t launch_norm(NormArgs a, hipStream_t stream)
         a.blocks = blocks_per_sample(a, rows * kNormUnroll);
         hipLaunchKernelGGL((k_norm_stats<T, V>), dim3(a.samples * a.blocks), dim3(kNormThreads), lds, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k_norm_merge<T>, dim3(a.samples * a.groups), dim3(64), 0, stream, a);
+        if (a.blocks <= 64 * kMergeEach)
+            hipLaunchKernelGGL(k_norm_merge<64>, dim3(a.samples * a.groups), dim3(64), 0, stream, a);
+        else
+            hipLaunchKernelGGL(k_norm_merge<256>, dim3(a.samples * a.groups), dim3(256), 0, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         hipLaunchKernelGGL((k_norm_apply<T, V, ACT>), dim3(a.samples * a.blocks), dim3(kNormThreads), 0, stream, a);
         return hipGetLastError();
@@ -463,8 +521,8 @@ hipError_t launch_norm(NormArgs a, hipStream_t stream)
         hipLaunchKernelGGL((k_norm_grad_sums<T, V, ACT>), dim3(a.samples * a.blocks), dim3(kNormThreads), lds, stream,
                            a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k_norm_grad_merge<T>, dim3(a.samples * (int)ceil_div(a.channels, 64)), dim3(kNormThreads),
-                           0, stream, a);
+        hipLaunchKernelGGL(k_norm_grad_merge, dim3(a.samples * (int)ceil_div(a.channels, kMergeChannels)),
+                           dim3(kMergeChannels * kMergeLanes), 0, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     } else {
         a.blocks = 1;
