@@ -86,6 +86,15 @@ __device__ __forceinline__ float activate_grad(float u)
     return 1.0f;
 }
 
+// The work that workgroup w of n takes: workgroups are dealt to the eight XCDs
+// in turn, so this gives each XCD a run of neighbours, which share lines of
+// its L2.
+__device__ __forceinline__ int xcd_order(int w, int n)
+{
+    const int each = n / 8, more = n % 8, x = w % 8;
+    return x * each + (x < more ? x : more) + w / 8;
+}
+
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }

@@ -174,52 +174,52 @@ struct Operand {
     }
 };
 
-// Workgroup w of n takes tile `at`: workgroups are dealt to the eight XCDs in
-// turn, so each XCD takes a run of neighbouring tiles, which share operands in
-// its L2.
-__device__ __forceinline__ int xcd_order(int w, int n)
-{
-    const int each = n / 8, more = n % 8, x = w % 8;
-    return x * each + (x < more ? x : more) + w / 8;
-}
-
-template <int ACT, typename T>
-__device__ __forceinline__ void finish(const GemmArgs &g, int m, int n, f32x4 v)
+// W neighbouring outputs of row m: bias, the value kept for the gradient,
+// activation, residual, each rounded once.
+template <int ACT, typename T, int W>
+__device__ __forceinline__ void finish(const GemmArgs &g, int m, int n, float (&v)[W])
 {
     const int left = g.n - n;
-    if (g.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (i < left) v[i] += g.bias[n + i];
-    }
     T *out = static_cast<T *>(g.out) + m * g.ldo + n;
     const T *res = g.residual ? static_cast<const T *>(g.residual) + m * g.ldr + n : nullptr;
     T *pre = g.preact ? static_cast<T *>(g.preact) + m * g.ldp + n : nullptr;
-    if (left >= 4) {
-        Vec<T, 4> o;
+    if (left >= W) {
+        Vec<T, W> o;
+        if (g.bias) {
+            const Vec<float, W> b = load_vec<float, W>(g.bias + n);
+#pragma unroll
+            for (int i = 0; i < W; i++) v[i] += b.v[i];
+        }
         if (pre) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) o.v[i] = (T)v[i];
-            store_vec<T, 4>(pre, o);
+            for (int i = 0; i < W; i++) o.v[i] = (T)v[i];
+            store_vec<T, W>(pre, o);
         }
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = activate<ACT>(v[i]);
+        for (int i = 0; i < W; i++) v[i] = activate<ACT>(v[i]);
         if (res) {
-            const Vec<T, 4> r = load_vec<T, 4>(res);
+            const Vec<T, W> r = load_vec<T, W>(res);
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[i] += (float)r.v[i];
+            for (int i = 0; i < W; i++) v[i] += (float)r.v[i];
         }
 #pragma unroll
-        for (int i = 0; i < 4; i++) o.v[i] = (T)v[i];
-        store_vec<T, 4>(out, o);
+        for (int i = 0; i < W; i++) o.v[i] = (T)v[i];
+        store_vec<T, W>(out, o);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int i = 0; i < W; i++)
             if (i < left) {
-                if (pre) pre[i] = (T)v[i];
-                out[i] = (T)(activate<ACT>(v[i]) + (res ? (float)res[i] : 0.0f));
+                const float z = v[i] + (g.bias ? g.bias[n + i] : 0.0f);
+                if (pre) pre[i] = (T)z;
+                out[i] = (T)(activate<ACT>(z) + (res ? (float)res[i] : 0.0f));
             }
     }
+}
+template <int ACT, typename T>
+__device__ __forceinline__ void finish(const GemmArgs &g, int m, int n, f32x4 v)
+{
+    float w[4] = {v[0], v[1], v[2], v[3]};
+    finish<ACT, T, 4>(g, m, n, w);
 }
 
 template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT>
@@ -366,6 +366,101 @@ __global__ __launch_bounds__(1024) void k_gemm_rows(GemmArgs g)
     }
 }
 
+// Narrow products (a map's projection to its embedding), whose B fits into LDS
+// whole: it is laid out there once per workgroup, along k, and the waves stream
+// the rows of A past it, 16 at a time, straight from memory into fragments, the
+// next strip in flight while the present one is multiplied.  No barrier and no
+// LDS traffic for A; every row is read once.
+//
+// B's rows within a pair of 16-row fragments are taken in the order
+// n = 8 (r / 4) + 4 t + r % 4 (fragment t, row r), which leaves each lane
+// eight neighbouring n of its row of A: one 16-byte store for 16-bit types.
+// Chunk c of row n lies at c ^ swizzle(n), so that eight lanes' reads meet all
+// the banks in that order.
+template <typename T>
+constexpr int kNarrowStep = 4 * kChunk<T>;       // k of one fragment
+constexpr int kNarrowLds = 64 << 10;             // most bytes of B
+__device__ __forceinline__ int narrow_swizzle(int n) { return (n & 3) | ((n >> 3) & 1) << 2; }
+
+template <typename T, int KS, bool B_ACROSS, int ACT>
+__global__ __launch_bounds__(256) void k_gemm_narrow(GemmArgs g)
+{
+    extern __shared__ __align__(1024) unsigned char narrow_lds[];
+    constexpr int E = kChunk<T>, kRow = KS * 4;        // chunks in a row of B
+    lds_byte *lds = (lds_byte *)narrow_lds;
+    const int pairs = (g.n + 31) / 32, n_pad = pairs * 32;
+    for (int q = threadIdx.x; q < n_pad * kRow; q += 256) {
+        int n, c;
+        Fragment f;
+        f.u = u32x4{0, 0, 0, 0};
+        if constexpr (B_ACROSS) {       // neighbouring threads read neighbouring n
+            c = q / n_pad;
+            n = q - c * n_pad;
+            T e[E];
+#pragma unroll
+            for (int i = 0; i < E; i++)
+                e[i] = n < g.n && c * E + i < g.k ? static_cast<const T *>(g.b)[(int64_t)(c * E + i) * g.ldb + n]
+                                                  : (T)0.0f;
+            __builtin_memcpy(&f, e, 16);
+        } else {
+            n = q / kRow;
+            c = q - n * kRow;
+            f.u = load_chunk<T>(static_cast<const T *>(g.b) + (int64_t)n * g.ldb + c * E, n < g.n ? g.k - c * E : 0);
+        }
+        *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const int strips = (g.m + 15) / 16, step = gridDim.x * 4;
+    const int full = g.k / E;                    // whole chunks of a row of A
+    auto fetch = [&](int strip, Fragment (&f)[KS]) {
+        const int m = strip * 16 + j;
+        const T *p = static_cast<const T *>(g.a) + m * g.lda;
+        const bool on = m < g.m;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            const int chunk = 4 * s + c;
+            f[s].u = u32x4{0, 0, 0, 0};
+            if (on && chunk < full) {
+                const Vec<T, E> v = load_vec<T, E>(p + chunk * E);
+                __builtin_memcpy(&f[s], &v, 16);
+            } else if (on && chunk == full) {
+                f[s].u = load_chunk<T>(p + chunk * E, g.k - chunk * E);
+            }
+        }
+    };
+    Fragment next[KS];
+    int strip = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (strip < strips) fetch(strip, next);
+    const int row = 8 * (j >> 2) + (j & 3);
+    for (; strip < strips; strip += step) {
+        Fragment fa[KS];
+#pragma unroll
+        for (int s = 0; s < KS; s++) fa[s] = next[s];
+        if (strip + step < strips) fetch(strip + step, next);
+        const int m = strip * 16 + j;
+        for (int p = 0; p < pairs; p++) {
+            f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+            for (int s = 0; s < KS; s++)
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    const int n = 32 * p + row + 4 * t;
+                    Fragment fb;
+                    fb.u = *(const __attribute__((address_space(3))) u32x4 *)(
+                        lds + (n * kRow + ((4 * s + c) ^ narrow_swizzle(n))) * 16);
+                    acc[t] = mma<T>(fb, fa[s], acc[t]);
+                }
+            const int n = 32 * p + 8 * c;
+            if (m < g.m && n < g.n) {
+                float v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3],
+                              acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+                finish<ACT, T, 8>(g, m, n, v);
+            }
+        }
+    }
+}
+
 // dz = dy act'(preact), rounded (the products' operand), and its column sums
 // over this workgroup's rows, unrounded.  A workgroup covers up to 256 vectors
 // of V columns (blockIdx.y) and 256 / vectors rows at a time.
@@ -504,10 +599,45 @@ hipError_t launch_rows(const GemmArgs &g, hipStream_t stream)
     return hipGetLastError();
 }
 
+// Fragments of k that hold a row of A (2, 4, 8 or 16), 0 where it is too long.
+template <typename T>
+int narrow_steps(int k)
+{
+    for (int ks = 2; ks <= 16; ks *= 2)
+        if (k <= ks * kNarrowStep<T>) return ks;
+    return 0;
+}
+template <typename T>
+int narrow_bytes(const GemmArgs &g)
+{
+    return (int)(ceil_div(g.n, 32) * 32 * narrow_steps<T>(g.k) * 64);
+}
+template <typename T>
+bool narrow_fits(const GemmArgs &g)
+{
+    return narrow_steps<T>(g.k) > 0 && g.n <= 4096 && narrow_bytes<T>(g) <= kNarrowLds;
+}
+
+template <typename T, bool B_ACROSS, int ACT>
+hipError_t launch_narrow(const GemmArgs &g, hipStream_t stream)
+{
+    const int bytes = narrow_bytes<T>(g), per_cu = (160 << 10) / (bytes + 1024);
+    const int64_t want = ceil_div(ceil_div(g.m, 16), 4), most = 256 * (per_cu < 4 ? per_cu : 4);
+    const dim3 grid((unsigned)(want < most ? want : most));
+    switch (narrow_steps<T>(g.k)) {
+    case 2: hipLaunchKernelGGL((k_gemm_narrow<T, 2, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
+    case 4: hipLaunchKernelGGL((k_gemm_narrow<T, 4, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
+    case 8: hipLaunchKernelGGL((k_gemm_narrow<T, 8, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
+    default: hipLaunchKernelGGL((k_gemm_narrow<T, 16, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
+    }
+    return hipGetLastError();
+}
+
 template <typename T, int ACT>
 hipError_t launch_forward(const GemmArgs &g, hipStream_t stream)
 {
     if (g.m <= 64) return launch_rows<T, ACT>(g, stream);
+    if (narrow_fits<T>(g)) return launch_narrow<T, false, ACT>(g, stream);
     return launch_tiles<T, false, false, ACT>(g, stream);
 }
 
@@ -526,7 +656,8 @@ hipError_t launch_gemm_type(const GemmArgs &all, hipStream_t stream)
         g.m = (int32_t)(all.m - m < most ? all.m - m : most);
         hipError_t e;
         if (g.b_cols)
-            e = launch_tiles<T, false, true, CPE_ACT_NONE>(g, stream);
+            e = narrow_fits<T>(g) ? launch_narrow<T, true, CPE_ACT_NONE>(g, stream)
+                                  : launch_tiles<T, false, true, CPE_ACT_NONE>(g, stream);
         else if (g.act == CPE_ACT_RELU)
             e = launch_forward<T, CPE_ACT_RELU>(g, stream);
         else if (g.act == CPE_ACT_SILU)

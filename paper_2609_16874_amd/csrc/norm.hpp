@@ -23,7 +23,8 @@ struct NormArgs {
     float *part;                        // scratch: [samples][blocks][G or C][2]
     float *chan;                        // scratch: [samples][C][2] (backward)
     float *dgamma, *dbeta;              // may be null
-    int32_t samples, pixels, channels, groups, blocks;
+    int32_t samples, pixels, channels, groups;
+    int32_t blocks, chunk;              // workgroups per sample, rows that each takes at a time
     float eps;
     int act;
     bool backward;

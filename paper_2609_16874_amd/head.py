@@ -13,10 +13,18 @@ from __future__ import annotations
 import ctypes
 from typing import Optional
 
-from .native import CPE_BF16, CPE_F16, CPE_F32, CPE_OK, CpeError, _stream_ptr, library, torch_dtype
+import torch
+
+from .native import CPE_BF16, CPE_F16, CPE_F32, CPE_OK, CpeError, library, torch_dtype
 
 DTYPES = {"f32": CPE_F32, "f16": CPE_F16, "bf16": CPE_BF16}
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def _stream(stream, device: int) -> int:
+    """The HIP stream's handle (the current one's without the stream object,
+    whose construction takes as long as the launch)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _need(ok: bool, what: str):
@@ -24,13 +32,12 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _vector(t, n: int, name: str, dtype=None):
-    """A contiguous device vector (float32 unless ``dtype``), or None."""
-    import torch
+def _vector(t, n: int, name: str, dtype=torch.float32):
+    """The pointer of a contiguous device vector, or None."""
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == (dtype or torch.float32) and t.numel() == n and t.is_contiguous(),
-          f"{name}: a contiguous device tensor of {n} {dtype or torch.float32} is needed")
+    if not (t.is_cuda and t.dtype is dtype and t.numel() == n and t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous device tensor of {n} {dtype} is needed")
     return t.data_ptr()
 
 
@@ -43,55 +50,58 @@ class GroupNorm:
     def __init__(self, max_samples: int, max_pixels: int, channels: int, groups: int, dtype: str,
                  activation: str = "none", eps: float = 1e-5):
         self.channels, self.groups, self.dtype = int(channels), int(groups), dtype
-        self._torch_dtype = torch_dtype(dtype)
+        self._torch_dtype, self._lib = torch_dtype(dtype), library()
         h = ctypes.c_void_p()
-        st = library().cpe_norm_create(ctypes.byref(h), int(max_samples), int(max_pixels), self.channels,
+        st = self._lib.cpe_norm_create(ctypes.byref(h), int(max_samples), int(max_pixels), self.channels,
                                        self.groups, DTYPES[dtype], ACTIVATIONS[activation], float(eps))
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_create")
-        self._h = h
+        self._h, self._device = h, torch.cuda.current_device()
 
-    def _map(self, t, name: str, shape=None):
+    def _map(self, t, name: str, size=None):
         """(pointer, pixel stride, sample stride, (samples, pixels)) of a map."""
-        if t.dim() == 4:
-            _need(t.shape[1] <= 1 or t.shape[2] == 0 or t.stride(1) == t.shape[2] * t.stride(2),
-                  f"{name}: image rows must follow one another")
-            size, ld = (t.shape[0], t.shape[1] * t.shape[2]), t.stride(2) if t.shape[2] > 1 else t.stride(1)
+        shape, strides = t.shape, t.stride()
+        if len(shape) == 3:
+            samples, pixels, channels = shape
+            ld = strides[1]
         else:
-            _need(t.dim() == 3, f"{name}: three or four dimensions, channels last")
-            size, ld = (t.shape[0], t.shape[1]), t.stride(1)
-        _need(t.is_cuda and t.dtype == self._torch_dtype and t.shape[-1] == self.channels
-              and (self.channels == 1 or t.stride(-1) == 1) and (shape is None or size == shape),
-              f"{name}: wrong shape, dtype, device or channel stride")
-        return t.data_ptr(), max(ld, self.channels) if size[1] <= 1 else ld, t.stride(0), size
+            _need(len(shape) == 4, f"{name}: three or four dimensions, channels last")
+            samples, height, width, channels = shape
+            pixels = height * width
+            _need(height <= 1 or width == 0 or strides[1] == width * strides[2],
+                  f"{name}: image rows must follow one another")
+            ld = strides[2] if width > 1 else strides[1]
+        if not (t.is_cuda and t.dtype is self._torch_dtype and channels == self.channels
+                and (channels == 1 or strides[-1] == 1) and (size is None or size == (samples, pixels))):
+            raise ValueError(f"{name}: wrong shape, dtype, device or channel stride")
+        if pixels <= 1 and ld < channels:      # the stride of a single pixel says nothing
+            ld = channels
+        return t.data_ptr(), ld, strides[0], (samples, pixels)
 
     def forward(self, x, gamma, beta, y, stats=None, valid=None, stream=None) -> int:
         """cpe_norm_forward: ``stats`` receives float32 [samples][G][2] for the
         gradient; ``valid`` holds int32 pixel counts, one per sample."""
-        import torch
         px, x_ld, x_sample, size = self._map(x, "x")
         py, y_ld, y_sample, _ = self._map(y, "y", size)
-        return library().cpe_norm_forward(
-            self._h, _stream_ptr(stream), size[0], size[1], px, x_ld, x_sample,
+        return self._lib.cpe_norm_forward(
+            self._h, _stream(stream, self._device), size[0], size[1], px, x_ld, x_sample,
             _vector(gamma, self.channels, "gamma"), _vector(beta, self.channels, "beta"),
             _vector(valid, size[0], "valid", torch.int32), py, y_ld, y_sample,
             _vector(stats, 2 * size[0] * self.groups, "stats"))
 
     def backward(self, x, dy, gamma, beta, stats, dx=None, dgamma=None, dbeta=None, valid=None, stream=None) -> int:
         """cpe_norm_backward: writes those of dx, dgamma and dbeta that are given."""
-        import torch
         px, x_ld, x_sample, size = self._map(x, "x")
         pd, dy_ld, dy_sample, _ = self._map(dy, "dy", size)
         po, dx_ld, dx_sample, _ = (None, 0, 0, None) if dx is None else self._map(dx, "dx", size)
-        return library().cpe_norm_backward(
-            self._h, _stream_ptr(stream), size[0], size[1], px, x_ld, x_sample, pd, dy_ld, dy_sample,
+        return self._lib.cpe_norm_backward(
+            self._h, _stream(stream, self._device), size[0], size[1], px, x_ld, x_sample, pd, dy_ld, dy_sample,
             _vector(gamma, self.channels, "gamma"), _vector(beta, self.channels, "beta"),
             _vector(valid, size[0], "valid", torch.int32), _vector(stats, 2 * size[0] * self.groups, "stats"),
             po, dx_ld, dx_sample, _vector(dgamma, self.channels, "dgamma"), _vector(dbeta, self.channels, "dbeta"))
 
     def run(self, x, gamma, beta, valid=None, stream=None):
         """forward into new tensors: (y, stats)."""
-        import torch
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         stats = torch.empty((x.shape[0], self.groups, 2), dtype=torch.float32, device=x.device)
         st = self.forward(x, gamma, beta, y, stats, valid, stream)
@@ -101,7 +111,6 @@ class GroupNorm:
 
     def run_backward(self, x, dy, gamma, beta, stats, valid=None, stream=None):
         """backward into new tensors: (dx, dgamma, dbeta)."""
-        import torch
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         dgamma, dbeta = (torch.empty(self.channels, dtype=torch.float32, device=x.device) for _ in range(2))
         st = self.backward(x, dy, gamma, beta, stats, dx, dgamma, dbeta, valid, stream)
@@ -110,11 +119,11 @@ class GroupNorm:
         return dx, dgamma, dbeta
 
     def workspace_bytes(self) -> int:
-        return int(library().cpe_norm_workspace_bytes(self._h))
+        return int(self._lib.cpe_norm_workspace_bytes(self._h))
 
     def close(self):
         if getattr(self, "_h", None):
-            library().cpe_norm_destroy(self._h)
+            self._lib.cpe_norm_destroy(self._h)
             self._h = None
 
     def __del__(self):
@@ -131,22 +140,24 @@ class Linear:
 
     def __init__(self, max_rows: int, in_features: int, out_features: int, dtype: str, activation: str = "none"):
         self.in_features, self.out_features, self.dtype = int(in_features), int(out_features), dtype
-        self._torch_dtype = torch_dtype(dtype)
+        self._torch_dtype, self._lib = torch_dtype(dtype), library()
         h = ctypes.c_void_p()
-        st = library().cpe_linear_create(ctypes.byref(h), int(max_rows), self.in_features, self.out_features,
+        st = self._lib.cpe_linear_create(ctypes.byref(h), int(max_rows), self.in_features, self.out_features,
                                          DTYPES[dtype], ACTIVATIONS[activation])
         if st != CPE_OK:
             raise CpeError(st, "cpe_linear_create")
-        self._h = h
+        self._h, self._device = h, torch.cuda.current_device()
 
     def _matrix(self, t, rows: Optional[int], width: int, name: str):
         """(pointer, row stride) of a matrix, (None, 0) for None."""
         if t is None:
             return None, 0
-        _need(t.is_cuda and t.dtype == self._torch_dtype and t.dim() == 2 and t.shape[1] == width
-              and (rows is None or t.shape[0] == rows) and (width == 1 or t.stride(1) == 1),
-              f"{name}: wrong shape, dtype, device or feature stride")
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+        shape, strides = t.shape, t.stride()
+        if not (len(shape) == 2 and t.is_cuda and t.dtype is self._torch_dtype and shape[1] == width
+                and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
+            raise ValueError(f"{name}: wrong shape, dtype, device or feature stride")
+        ld = strides[0]
+        return t.data_ptr(), width if shape[0] <= 1 and ld < width else ld
 
     def forward(self, x, weight, bias, y, residual=None, preact=None, stream=None) -> int:
         """cpe_linear_forward: ``preact`` receives the value before the
@@ -157,7 +168,7 @@ class Linear:
         py, y_ld = self._matrix(y, rows, n, "y")
         pr, r_ld = self._matrix(residual, rows, n, "residual")
         pz, z_ld = self._matrix(preact, rows, n, "preact")
-        return library().cpe_linear_forward(self._h, _stream_ptr(stream), rows, px, x_ld, pw, w_ld,
+        return self._lib.cpe_linear_forward(self._h, _stream(stream, self._device), rows, px, x_ld, pw, w_ld,
                                             _vector(bias, n, "bias"), pr, r_ld, py, y_ld, pz, z_ld)
 
     def backward(self, x, weight, dy, preact=None, dx=None, dweight=None, dbias=None, stream=None) -> int:
@@ -169,12 +180,11 @@ class Linear:
         pz, z_ld = self._matrix(preact, rows, n, "preact")
         po, o_ld = self._matrix(dx, rows, k, "dx")
         pg, g_ld = self._matrix(dweight, n, k, "dweight")
-        return library().cpe_linear_backward(self._h, _stream_ptr(stream), rows, px, x_ld, pw, w_ld, pd, d_ld,
+        return self._lib.cpe_linear_backward(self._h, _stream(stream, self._device), rows, px, x_ld, pw, w_ld, pd, d_ld,
                                              pz, z_ld, po, o_ld, pg, g_ld, _vector(dbias, n, "dbias"))
 
     def run(self, x, weight, bias=None, residual=None, keep=False, stream=None):
         """forward into new tensors: y, or (y, preact) where ``keep``."""
-        import torch
         y = torch.empty((x.shape[0], self.out_features), dtype=x.dtype, device=x.device)
         preact = torch.empty_like(y) if keep else None
         st = self.forward(x, weight, bias, y, residual, preact, stream)
@@ -184,7 +194,6 @@ class Linear:
 
     def run_backward(self, x, weight, dy, preact=None, stream=None):
         """backward into new tensors: (dx, dweight, dbias)."""
-        import torch
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         dweight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
         dbias = torch.empty(self.out_features, dtype=torch.float32, device=x.device)
@@ -194,11 +203,11 @@ class Linear:
         return dx, dweight, dbias
 
     def workspace_bytes(self) -> int:
-        return int(library().cpe_linear_workspace_bytes(self._h))
+        return int(self._lib.cpe_linear_workspace_bytes(self._h))
 
     def close(self):
         if getattr(self, "_h", None):
-            library().cpe_linear_destroy(self._h)
+            self._lib.cpe_linear_destroy(self._h)
             self._h = None
 
     def __del__(self):
