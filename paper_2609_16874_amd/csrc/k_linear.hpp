@@ -39,8 +39,6 @@ constexpr int kChunk = 16 / (int)sizeof(T);           // elements in 16 bytes
 template <typename T>
 constexpr int kStepK = 8 * kChunk<T>;                 // k of one LDS tile
 
-__device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
-
 union Fragment {
     u32x4 u;
     f16x8 h;
@@ -48,6 +46,9 @@ union Fragment {
     f32x4 f;
     s16x4 s[2];
 };
+
+// The first thread of this wave, as a scalar.
+__device__ __forceinline__ int wave_base() { return __builtin_amdgcn_readfirstlane(threadIdx.x & ~63); }
 
 template <typename T>
 __device__ __forceinline__ f32x4 mma(const Fragment &n, const Fragment &m, f32x4 acc)
@@ -81,61 +82,79 @@ __device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left)
     return f.u;
 }
 
-// One operand of a workgroup: R rows (m or n) by kStepK of k.
-template <typename T, bool ACROSS, int R, bool DIRECT>
+// One operand of a workgroup: R rows (m or n) by kStepK of k.  DIRECT: loads
+// through a buffer descriptor straight into LDS; a lane out of range has an
+// offset beyond the descriptor's, which reads as 0.
+constexpr uint32_t kBufferBytes = 0x80000000u;
+template <typename T, bool ACROSS, bool DIRECT>
 struct Operand {
-    static constexpr int E = kChunk<T>, kLoads = R * 8 / kGemmThreads;
+    static constexpr int E = kChunk<T>, R = kTile, kLoads = R * 8 / kGemmThreads;
     static constexpr int kPerRow = ACROSS ? R / E : 8;    // chunks in an LDS row
     static constexpr int kBytes = R * 128;
-    const T *src[kLoads];
-    int room[kLoads];       // along k: k left from this chunk on; across: valid elements of the chunk
-    int krow[kLoads];       // across: k of the chunk
+    static constexpr int kReads = !ACROSS ? 1 : sizeof(T) == 4 ? 4 : 2;      // LDS reads of a fragment
+    const T *base;          // DIRECT: of the workgroup; else of the first row
     int64_t step;
+    uint32_t off[kLoads];   // DIRECT: bytes from the base
+    const T *src[DIRECT ? 1 : kLoads];
+    int room[DIRECT ? 1 : kLoads];      // staged, across: valid elements of the chunk
     u32x4 held[DIRECT ? 1 : kLoads];
 
     __device__ __forceinline__ static int permute(int krow)      // of the 32-byte units of a row across k
     {
         if constexpr (sizeof(T) == 4) return 0;
-        return R >= 128 ? (krow & 3) | ((krow >> 3) & 1) << 2 : ((krow >> 1) & 1) | ((krow >> 3) & 1) << 1;
+        return (krow & 3) | ((krow >> 3) & 1) << 2;
+    }
+    // this thread's i-th chunk: its row in LDS, and the chunk of the row
+    __device__ __forceinline__ static int row_of(int i) { return (i * kGemmThreads + threadIdx.x) / kPerRow; }
+    __device__ __forceinline__ static int chunk_of(int i)
+    {
+        const int pc = (i * kGemmThreads + threadIdx.x) % kPerRow, row = row_of(i);
+        if constexpr (!ACROSS) return pc ^ (row & 7);
+        return sizeof(T) == 4 ? pc : ((((pc >> 1) ^ permute(row)) << 1) | (pc & 1));
     }
 
-    __device__ __forceinline__ void init(const void *base, int64_t ld, int r0, int r_end, int k0)
+    __device__ __forceinline__ void init(const void *p, int64_t ld, int r0, int r_end, int k0)
     {
         step = ACROSS ? kStepK<T> * ld : kStepK<T>;
-        const T *p = static_cast<const T *>(base);
+        base = static_cast<const T *>(p) + (ACROSS ? k0 * ld + r0 : r0 * ld + k0);
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const int q = i * kGemmThreads + threadIdx.x, row = q / kPerRow, pc = q % kPerRow;
-            if constexpr (ACROSS) {
-                const int lc = sizeof(T) == 4 ? pc : ((((pc >> 1) ^ permute(row)) << 1) | (pc & 1));
-                const int r = r0 + lc * E;
-                krow[i] = row;
-                room[i] = r_end - r;
-                src[i] = room[i] > 0 ? p + (int64_t)(k0 + row) * ld + r : nullptr;
+            const int row = row_of(i), c = chunk_of(i);
+            const int left = ACROSS ? r_end - r0 - c * E : r_end - r0 - row;
+            if constexpr (DIRECT) {
+                off[i] = left > 0 ? (uint32_t)((row * ld + c * E) * (int64_t)sizeof(T)) : kBufferBytes;
             } else {
-                const int lc = pc ^ (row & 7);
-                room[i] = lc * E;
-                krow[i] = 0;
-                src[i] = r0 + row < r_end ? p + (int64_t)(r0 + row) * ld + k0 + lc * E : nullptr;
+                room[i] = left;
+                src[i] = base + row * ld + c * E;
             }
         }
     }
 
-    // Fetch the step with `left` k remaining: into LDS, or into registers.
+    // Fetch the next step into LDS, or into registers; TAIL: only `left` k of
+    // it exist.
+    template <bool TAIL>
     __device__ __forceinline__ void fetch(lds_byte *lds, int left)
     {
+        if constexpr (DIRECT) {
+#ifdef __HIP_DEVICE_COMPILE__       // (the host's pass does not know the descriptor's type)
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, (int)kBufferBytes, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int valid = src[i] == nullptr ? 0 : ACROSS ? (krow[i] < left ? room[i] : 0) : left - room[i];
-            if constexpr (DIRECT) {
-                const void *p = valid > 0 ? (const void *)src[i] : (const void *)zero_chunk;
-                lds_byte *to = lds + (i * kGemmThreads + (threadIdx.x & ~63)) * 16;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p,
-                                                 (__attribute__((address_space(3))) uint32_t *)to, 16, 0, 0);
-            } else {
-                held[i] = load_chunk<T>(src[i], valid);
+            for (int i = 0; i < kLoads; i++) {
+                uint32_t at = off[i];
+                if constexpr (TAIL) at = (ACROSS ? row_of(i) : chunk_of(i) * E) < left ? at : kBufferBytes;
+                lds_byte *to = lds + (i * kGemmThreads + wave_base()) * 16;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void *)to, 16, at,
+                                                         0, 0, 0);
             }
-            if (src[i]) src[i] += step;
+#endif
+            base += step;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) {
+                held[i] = load_chunk<T>(src[i], ACROSS ? (row_of(i) < left ? room[i] : 0)
+                                                       : (room[i] > 0 ? left - chunk_of(i) * E : 0));
+                src[i] += step;
+            }
         }
     }
     __device__ __forceinline__ void commit(lds_byte *lds) const
@@ -222,100 +241,201 @@ __device__ __forceinline__ void finish(const GemmArgs &g, int m, int n, f32x4 v)
     finish<ACT, T, 4>(g, m, n, w);
 }
 
-template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT>
-__global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs g)
+// Wait until no LDS read is in flight, and (LOADS) no load either.  (The fields
+// of s_waitcnt: loads in bits 0-3 and 14-15, LDS in 8-11, the rest idle.)
+template <bool LOADS>
+__device__ __forceinline__ void wait_for_lds()
 {
-    using A = Operand<T, A_ACROSS, kTile, DIRECT>;
-    using B = Operand<T, B_ACROSS, kTile, DIRECT>;
-    __shared__ __align__(1024) unsigned char smem[2][A::kBytes + B::kBytes];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(LOADS ? 0x0070 : 0xc07f);
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The order of a half step: LDS reads, then loads, one between two matrix
+// instructions each, so that neither waits for the other's unit.
+template <int READS, int LOADS, int MULTIPLIES>
+__device__ __forceinline__ void interleave()
+{
+    constexpr int kMfma = 0x8, kVmem = 0x20, kLdsRead = 0x100;
+#pragma unroll
+    for (int i = 0; i < READS; i++) {
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
+        if (i < MULTIPLIES) __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+        __builtin_amdgcn_sched_group_barrier(kVmem, 1, 0);
+        if (READS + i < MULTIPLIES) __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    }
+    if constexpr (MULTIPLIES > READS + LOADS)
+        __builtin_amdgcn_sched_group_barrier(kMfma, MULTIPLIES - READS - LOADS, 0);
+}
+
+// Tiles of 128 x 128 outputs, a wave for each 64 x 64 of them, two LDS tiles of
+// kStepK k, two workgroups per CU.  A step's two halves of fragments alternate
+// in registers: the second half is read while the first is multiplied, then
+// the waves meet and read the next step's first half while the second is
+// multiplied.  At the meeting the next step's LDS tile has arrived (DIRECT: its
+// loads went straight to LDS) and every wave has read the present one, whose
+// place the loads of the step after next take from then on.
+//
+// The epilogue passes through LDS, a row's 16-byte chunks permuted by the
+// row, so that every row leaves as whole lines and the code that finishes a
+// vector is there once.
+constexpr int kBand = 8;
+template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT>
+__global__ __launch_bounds__(kGemmThreads, 2) void k_gemm(GemmArgs g)
+{
+    using A = Operand<T, A_ACROSS, DIRECT>;
+    using B = Operand<T, B_ACROSS, DIRECT>;
+    constexpr int kStage = A::kBytes + B::kBytes, W = kTile / 32;       // fragments of a wave's rows
+    __shared__ __align__(1024) unsigned char smem[2 * kStage];
+    static_assert(2 * kStage >= kTile * kTile * 4, "the epilogue's tile fits");
     const int tiles = g.tiles_m * g.tiles_n;
     const int split = blockIdx.x / tiles, tile = xcd_order(blockIdx.x - split * tiles, tiles);
-    const int m0 = (tile / g.tiles_n) * kTile, n0 = (tile % g.tiles_n) * kTile;
+    // bands of eight rows of tiles, down then across: tiles at work together
+    // share both operands in the XCD's L2
+    const int band = tile / (kBand * g.tiles_n), in_band = tile - band * kBand * g.tiles_n;
+    const int high = g.tiles_m - band * kBand < kBand ? g.tiles_m - band * kBand : kBand;
+    const int m0 = (band * kBand + in_band % high) * kTile, n0 = in_band / high * kTile;
     const int k0 = split * g.k_split;
     const int len = g.k - k0 < g.k_split ? g.k - k0 : g.k_split;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int steps = len > 0 ? (len + kStepK<T> - 1) / kStepK<T> : 0;
+    const int whole = len / kStepK<T>;      // steps without a tail
+    const int wave = wave_base() >> 6, lane = threadIdx.x & 63;
     const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    lds_byte *lds = (lds_byte *)smem;
     A a;
     B b;
     a.init(g.a, g.lda, m0, g.m, k0);
     b.init(g.b, g.ldb, n0, g.n, k0);
-    f32x4 acc[4][4];
+    f32x4 acc[W][W];
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < W; i++)
 #pragma unroll
-        for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto buffer = [&](int s) { return (lds_byte *)smem[s]; };
-    if (len > 0) {
-        a.fetch(buffer(0), len);
-        b.fetch(buffer(0) + A::kBytes, len);
-        a.commit(buffer(0));
-        b.commit(buffer(0) + A::kBytes);
+        for (int j = 0; j < W; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto fetch = [&](auto tail, int step) __attribute__((always_inline)) {
+        constexpr bool TAIL = decltype(tail)::value;
+        lds_byte *to = lds + (step & 1) * kStage;
+        a.template fetch<TAIL>(to, len - step * kStepK<T>);
+        b.template fetch<TAIL>(to + A::kBytes, len - step * kStepK<T>);
+    };
+    auto fetch_any = [&](int step) __attribute__((always_inline)) {
+        if (step < whole)
+            fetch(std::false_type{}, step);
+        else
+            fetch(std::true_type{}, step);
+    };
+    auto commit = [&](int step) {
+        a.commit(lds + (step & 1) * kStage);
+        b.commit(lds + (step & 1) * kStage + A::kBytes);
+    };
+    Fragment fa[2][W], fb[2][W];
+    auto read = [&](int step, int half) {
+        const lds_byte *la = lds + (step & 1) * kStage, *lb = la + A::kBytes;
+#pragma unroll
+        for (int i = 0; i < W; i++) fa[half][i] = A::read(la, wm + 16 * i, half);
+#pragma unroll
+        for (int j = 0; j < W; j++) fb[half][j] = B::read(lb, wn + 16 * j, half);
+    };
+    auto multiply = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < W; i++)
+#pragma unroll
+            for (int j = 0; j < W; j++) acc[i][j] = mma<T>(fb[half][j], fa[half][i], acc[i][j]);
+    };
+    constexpr int kReads = W * (A::kReads + B::kReads), kMultiplies = W * W * (sizeof(T) == 4 ? 4 : 1);
+    if (steps > 0) {
+        fetch_any(0);
+        commit(0);
+        wait_for_lds<true>();
+        meet();
+        read(0, 0);
     }
-    int cur = 0;
-    for (int left = len; left > 0; left -= kStepK<T>, cur ^= 1) {
-        __syncthreads();
-        const bool more = left > kStepK<T>;
-        if (more) {
-            a.fetch(buffer(cur ^ 1), left - kStepK<T>);
-            b.fetch(buffer(cur ^ 1) + A::kBytes, left - kStepK<T>);
-        }
-        const lds_byte *la = buffer(cur), *lb = la + A::kBytes;
-#pragma unroll
-        for (int s = 0; s < 2; s++) {
-            Fragment fa[4], fb[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) fa[i] = A::read(la, wm + 16 * i, s);
-#pragma unroll
-            for (int i = 0; i < 4; i++) fb[i] = B::read(lb, wn + 16 * i, s);
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
-        }
-        if (more) {
-            a.commit(buffer(cur ^ 1));
-            b.commit(buffer(cur ^ 1) + A::kBytes);
-        }
+    int t = 0;
+    for (; t + 1 < whole; t++) {        // the steps whose loads are whole: no branch
+        wait_for_lds<false>();          // the fragments of the first half
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(std::false_type{}, t + 1);
+        read(t, 1);
+        multiply(0);
+        interleave<kReads, DIRECT ? A::kLoads + B::kLoads : 0, kMultiplies>();
+        __builtin_amdgcn_sched_barrier(0);
+        commit(t + 1);
+        wait_for_lds<true>();
+        meet();
+        __builtin_amdgcn_sched_barrier(0);
+        read(t + 1, 0);
+        multiply(1);
+        interleave<kReads, 0, kMultiplies>();
+        __builtin_amdgcn_sched_barrier(0);
     }
+    for (; t < steps; t++) {
+        const bool more = t + 1 < steps;
+        if (more) fetch_any(t + 1);
+        read(t, 1);
+        multiply(0);
+        if (more) commit(t + 1);
+        wait_for_lds<true>();
+        meet();
+        if (more) read(t + 1, 0);
+        multiply(1);
+    }
+    // no load is in flight, and every wave has read its last fragments
+    typedef __attribute__((address_space(3))) f32x4 lds_quad;
+    auto place = [&](int m, int n) { return (lds_quad *)(lds + (m * (kTile / 4) + ((n >> 2) ^ (m & 15))) * 16); };
+#pragma unroll
+    for (int i = 0; i < W; i++)
+#pragma unroll
+        for (int j = 0; j < W; j++) *place(wm + 16 * i + (lane & 15), wn + 16 * j + 4 * (lane >> 4)) = acc[i][j];
+    __syncthreads();
     const int64_t ldpart = (g.n + 3) / 4 * 4;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int m = m0 + wm + 16 * i + (lane & 15);
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
-            if (m >= g.m || n >= g.n) continue;
-            if (g.splits > 1)
-                *reinterpret_cast<f32x4 *>(g.part + ((int64_t)split * g.m + m) * ldpart + n) = acc[i][j];
-            else
-                finish<ACT, T>(g, m, n, acc[i][j]);
+    for (int q = threadIdx.x; q < kTile * kTile / 8; q += kGemmThreads) {
+        const int r = q / (kTile / 8), c = q % (kTile / 8) * 8, m = m0 + r, n = n0 + c;
+        if (m >= g.m || n >= g.n) continue;
+        const f32x4 v0 = *place(r, c), v1 = *place(r, c + 4);
+        if (g.splits > 1) {
+            float *p = g.part + ((int64_t)split * g.m + m) * ldpart + n;
+            *reinterpret_cast<f32x4 *>(p) = v0;
+            if (n + 4 < g.n) *reinterpret_cast<f32x4 *>(p + 4) = v1;
+        } else {
+            float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            finish<ACT, T, 8>(g, m, n, v);
         }
     }
 }
 
 // The splits' partial products summed in a fixed order, then the epilogue:
-// 16 vectors of four n per workgroup, 16 lanes of splits for each.
-template <typename T, int ACT>
+// LANES neighbours-by-256/LANES share a vector of four n where there are many
+// splits.
+template <typename T, int LANES, int ACT>
 __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g)
 {
-    __shared__ f32x4 lds[4][16];
-    const int quads = (g.n + 3) / 4, at = threadIdx.x & 15, lane = threadIdx.x >> 4;
-    const int64_t all = (int64_t)g.m * quads, q = (int64_t)blockIdx.x * 16 + at;
+    constexpr int kVectors = 256 / LANES;
+    __shared__ f32x4 lds[LANES][kVectors];
+    const int quads = (g.n + 3) / 4, at = threadIdx.x % kVectors, lane = threadIdx.x / kVectors;
+    const int64_t all = (int64_t)g.m * quads, q = (int64_t)blockIdx.x * kVectors + at;
     const int64_t step = all * 4;
     const float *p = g.part + q * 4;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (q < all) {
 #pragma unroll 4
-        for (int s = lane; s < g.splits; s += 16) v += *reinterpret_cast<const f32x4 *>(p + s * step);
+        for (int s = lane; s < g.splits; s += LANES) v += *reinterpret_cast<const f32x4 *>(p + s * step);
     }
+    if constexpr (LANES > 1) {
+        lds[lane][at] = v;
+        __syncthreads();
+        if (lane > 0) return;
 #pragma unroll
-    for (int o = 16; o <= 32; o <<= 1)
-#pragma unroll
-        for (int i = 0; i < 4; i++) v[i] += __shfl_xor(v[i], o);
-    if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][at] = v;
-    __syncthreads();
-    if (threadIdx.x < 16 && q < all) {
-        v = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
+        for (int l = 1; l < LANES; l++) v += lds[l][at];
+    }
+    if (q < all) {
         const int m = (int)(q / quads);
         finish<ACT, T>(g, m, (int)(q - (int64_t)m * quads) * 4, v);
     }
@@ -382,51 +502,56 @@ constexpr int kNarrowStep = 4 * kChunk<T>;       // k of one fragment
 constexpr int kNarrowLds = 64 << 10;             // most bytes of B
 __device__ __forceinline__ int narrow_swizzle(int n) { return (n & 3) | ((n >> 3) & 1) << 2; }
 
-template <typename T, int KS, bool B_ACROSS, int ACT>
-__global__ __launch_bounds__(256) void k_gemm_narrow(GemmArgs g)
+// FULL: k fills the fragments.  Otherwise a row's last chunk is its last 16
+// bytes, the elements that the chunk before has too masked to 0 (in B as well),
+// and chunks beyond it are 0: no load leaves the row, and none is conditional.
+template <typename T, int KS, bool FULL, bool B_ACROSS, int ACT>
+__global__ __launch_bounds__(256, KS <= 8 ? 4 : 2) void k_gemm_narrow(GemmArgs g)
 {
     extern __shared__ __align__(1024) unsigned char narrow_lds[];
     constexpr int E = kChunk<T>, kRow = KS * 4;        // chunks in a row of B
     lds_byte *lds = (lds_byte *)narrow_lds;
     const int pairs = (g.n + 31) / 32, n_pad = pairs * 32;
+    // the first element of chunk c, and how many of its elements are not its own
+    auto start = [&](int c) { return FULL || c * E <= g.k - E ? c * E : g.k - E; };
+    auto extra = [&](int c) { return c * E - start(c); };
     for (int q = threadIdx.x; q < n_pad * kRow; q += 256) {
         int n, c;
-        Fragment f;
-        f.u = u32x4{0, 0, 0, 0};
+        T e[E];
         if constexpr (B_ACROSS) {       // neighbouring threads read neighbouring n
             c = q / n_pad;
             n = q - c * n_pad;
-            T e[E];
-#pragma unroll
-            for (int i = 0; i < E; i++)
-                e[i] = n < g.n && c * E + i < g.k ? static_cast<const T *>(g.b)[(int64_t)(c * E + i) * g.ldb + n]
-                                                  : (T)0.0f;
-            __builtin_memcpy(&f, e, 16);
         } else {
             n = q / kRow;
             c = q - n * kRow;
-            f.u = load_chunk<T>(static_cast<const T *>(g.b) + (int64_t)n * g.ldb + c * E, n < g.n ? g.k - c * E : 0);
         }
+        const int k0 = start(c), skip = n < g.n ? extra(c) : E;
+        const T *p = static_cast<const T *>(g.b) + (B_ACROSS ? (int64_t)k0 * g.ldb + n : (int64_t)n * g.ldb + k0);
+#pragma unroll
+        for (int i = 0; i < E; i++) e[i] = i >= skip ? p[B_ACROSS ? i * g.ldb : i] : (T)0.0f;
+        Fragment f;
+        __builtin_memcpy(&f, e, 16);
         *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
     const int strips = (g.m + 15) / 16, step = gridDim.x * 4;
-    const int full = g.k / E;                    // whole chunks of a row of A
     auto fetch = [&](int strip, Fragment (&f)[KS]) {
-        const int m = strip * 16 + j;
-        const T *p = static_cast<const T *>(g.a) + m * g.lda;
-        const bool on = m < g.m;
+        const int m = strip * 16 + j;           // rows beyond the last repeat it; they are not stored
+        const T *p = static_cast<const T *>(g.a) + (m < g.m ? m : g.m - 1) * g.lda;
 #pragma unroll
         for (int s = 0; s < KS; s++) {
-            const int chunk = 4 * s + c;
-            f[s].u = u32x4{0, 0, 0, 0};
-            if (on && chunk < full) {
-                const Vec<T, E> v = load_vec<T, E>(p + chunk * E);
-                __builtin_memcpy(&f[s], &v, 16);
-            } else if (on && chunk == full) {
-                f[s].u = load_chunk<T>(p + chunk * E, g.k - chunk * E);
-            }
+            const Vec<T, E> v = load_vec<T, E>(p + start(4 * s + c));
+            __builtin_memcpy(&f[s], &v, 16);
+        }
+    };
+    auto mask = [&](Fragment &f, int skip) {
+#pragma unroll
+        for (int d = 0; d < 4; d++) {
+            if constexpr (sizeof(T) == 4)
+                f.u[d] = d >= skip ? f.u[d] : 0u;
+            else
+                f.u[d] &= (2 * d >= skip ? 0xffffu : 0u) | (2 * d + 1 >= skip ? 0xffff0000u : 0u);
         }
     };
     Fragment next[KS];
@@ -436,7 +561,10 @@ __global__ __launch_bounds__(256) void k_gemm_narrow(GemmArgs g)
     for (; strip < strips; strip += step) {
         Fragment fa[KS];
 #pragma unroll
-        for (int s = 0; s < KS; s++) fa[s] = next[s];
+        for (int s = 0; s < KS; s++) {
+            fa[s] = next[s];
+            if constexpr (!FULL) mask(fa[s], extra(4 * s + c));
+        }
         if (strip + step < strips) fetch(strip + step, next);
         const int m = strip * 16 + j;
         for (int p = 0; p < pairs; p++) {
@@ -544,27 +672,33 @@ template <typename T>
 bool direct_ok(const GemmArgs &g)
 {
     constexpr int E = kChunk<T>;
-    auto ok = [](const void *p, int64_t ld, int width) {
-        return aligned_to(p, 16) && ld % E == 0 && width % E == 0;
+    auto ok = [](const void *p, int64_t ld, int width) {     // (a tile's offsets stay in the buffer)
+        return aligned_to(p, 16) && ld % E == 0 && width % E == 0 && ld < (int64_t)kBufferBytes / 2048;
     };
     return ok(g.a, g.lda, g.a_cols ? g.m : g.k) && ok(g.b, g.ldb, g.b_cols ? g.n : g.k);
 }
 
-// Workgroups dividing k where the tiles alone leave most of the chip idle:
-// at most kSplitTiles partial tiles, each of four steps of k or more.
+// Workgroups dividing k where the tiles alone leave half or more of the chip
+// empty.  A split's partial tiles are written, read again and joined in a
+// launch of their own, 5 us or more: so each split has at least kLeast steps
+// (bf16 2048 x 1024 to 512: 11 us in one piece, 22 in splits of four steps;
+// binary32 steps take four times as long), and the splits fill one place per
+// CU, both places only where 2 kLeast steps are left to each (1936 x 4096 to
+// 1024: 35 us on 512 places, 40 on 256, 53 in one piece).
 template <typename T>
 void choose_splits(GemmArgs &g)
 {
-    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n, steps = ceil_div(g.k, kStepK<T>);
-    int64_t splits = 1;
-    if (g.part && tiles <= kSplitTiles / 4) {
-        splits = kSplitTiles / tiles;
-        if (splits > steps / 4) splits = steps / 4;
-        if (splits < 1) splits = 1;
+    constexpr int kLeast = sizeof(T) == 4 ? 4 : 8;
+    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n, steps = g.k > 0 ? ceil_div(g.k, kStepK<T>) : 1;
+    int64_t splits = kSplitTiles / tiles;
+    if (splits > 1 && steps / splits < 2 * kLeast) {
+        splits = kSplitTiles / 2 / tiles;
+        if (splits > steps / kLeast) splits = steps / kLeast;
     }
-    const int64_t each = ceil_div(steps > 0 ? steps : 1, splits);
+    if (splits < 1) splits = 1;
+    const int64_t each = ceil_div(steps, splits);
     g.k_split = (int32_t)(each * kStepK<T>);
-    g.splits = (int32_t)ceil_div(steps > 0 ? steps : 1, each);
+    g.splits = (int32_t)ceil_div(steps, each);
 }
 
 template <typename T, bool A_ACROSS, bool B_ACROSS, int ACT>
@@ -580,7 +714,10 @@ hipError_t launch_tiles(GemmArgs g, hipStream_t stream)
         hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, false, ACT>), grid, dim3(kGemmThreads), 0, stream, g);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || g.splits == 1) return e;
     const int64_t quads = (int64_t)g.m * ((g.n + 3) / 4);
-    hipLaunchKernelGGL((k_gemm_join<T, ACT>), dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, stream, g);
+    if (g.splits <= 8)
+        hipLaunchKernelGGL((k_gemm_join<T, 1, ACT>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, stream, g);
+    else
+        hipLaunchKernelGGL((k_gemm_join<T, 16, ACT>), dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, stream, g);
     return hipGetLastError();
 }
 
@@ -615,20 +752,28 @@ int narrow_bytes(const GemmArgs &g)
 template <typename T>
 bool narrow_fits(const GemmArgs &g)
 {
-    return narrow_steps<T>(g.k) > 0 && g.n <= 4096 && narrow_bytes<T>(g) <= kNarrowLds;
+    return g.k >= kChunk<T> && narrow_steps<T>(g.k) > 0 && g.n <= 4096 && narrow_bytes<T>(g) <= kNarrowLds;
 }
 
 template <typename T, bool B_ACROSS, int ACT>
 hipError_t launch_narrow(const GemmArgs &g, hipStream_t stream)
 {
-    const int bytes = narrow_bytes<T>(g), per_cu = (160 << 10) / (bytes + 1024);
-    const int64_t want = ceil_div(ceil_div(g.m, 16), 4), most = 256 * (per_cu < 4 ? per_cu : 4);
+    // as many workgroups as run at once, by LDS and registers
+    const int bytes = narrow_bytes<T>(g), by_lds = (160 << 10) / bytes, by_regs = narrow_steps<T>(g.k) <= 8 ? 4 : 2;
+    const int64_t want = ceil_div(ceil_div(g.m, 16), 4), most = 256 * (by_lds < by_regs ? by_lds : by_regs);
     const dim3 grid((unsigned)(want < most ? want : most));
+    auto launch = [&](auto steps) {
+        constexpr int KS = decltype(steps)::value;
+        if (g.k == KS * kNarrowStep<T>)
+            hipLaunchKernelGGL((k_gemm_narrow<T, KS, true, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g);
+        else
+            hipLaunchKernelGGL((k_gemm_narrow<T, KS, false, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g);
+    };
     switch (narrow_steps<T>(g.k)) {
-    case 2: hipLaunchKernelGGL((k_gemm_narrow<T, 2, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
-    case 4: hipLaunchKernelGGL((k_gemm_narrow<T, 4, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
-    case 8: hipLaunchKernelGGL((k_gemm_narrow<T, 8, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
-    default: hipLaunchKernelGGL((k_gemm_narrow<T, 16, B_ACROSS, ACT>), grid, dim3(256), bytes, stream, g); break;
+    case 2: launch(std::integral_constant<int, 2>{}); break;
+    case 4: launch(std::integral_constant<int, 4>{}); break;
+    case 8: launch(std::integral_constant<int, 8>{}); break;
+    default: launch(std::integral_constant<int, 16>{}); break;
     }
     return hipGetLastError();
 }
