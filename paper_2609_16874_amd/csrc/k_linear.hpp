@@ -487,10 +487,11 @@ __global__ __launch_bounds__(1024) void k_gemm_rows(GemmArgs g)
 }
 
 // Narrow products (a map's projection to its embedding), whose B fits into LDS
-// whole: it is laid out there once per workgroup, along k, and the waves stream
-// the rows of A past it, 16 at a time, straight from memory into fragments, the
-// next strip in flight while the present one is multiplied.  No barrier and no
-// LDS traffic for A; every row is read once.
+// whole: it is laid out there once per workgroup, along k, and the workgroup
+// streams strips of 64 MT rows of A past it, each read once, in whole lines,
+// with the next strip's loads in flight.  A strip passes through LDS only to
+// turn its rows into fragments: once the waves have theirs (16 MT rows each)
+// its place is free again.
 //
 // B's rows within a pair of 16-row fragments are taken in the order
 // n = 8 (r / 4) + 4 t + r % 4 (fragment t, row r), which leaves each lane
@@ -500,17 +501,20 @@ __global__ __launch_bounds__(1024) void k_gemm_rows(GemmArgs g)
 template <typename T>
 constexpr int kNarrowStep = 4 * kChunk<T>;       // k of one fragment
 constexpr int kNarrowLds = 64 << 10;             // most bytes of B
+constexpr int narrow_tiles(int ks) { return ks >= 8 ? 1 : 8 / ks; }             // MT
+constexpr int narrow_strip_bytes(int ks) { return 64 * narrow_tiles(ks) * ks * 64; }
 __device__ __forceinline__ int narrow_swizzle(int n) { return (n & 3) | ((n >> 3) & 1) << 2; }
 
 // FULL: k fills the fragments.  Otherwise a row's last chunk is its last 16
 // bytes, the elements that the chunk before has too masked to 0 (in B as well),
 // and chunks beyond it are 0: no load leaves the row, and none is conditional.
 template <typename T, int KS, bool FULL, bool B_ACROSS, int ACT>
-__global__ __launch_bounds__(256, KS <= 8 ? 4 : 2) void k_gemm_narrow(GemmArgs g)
+__global__ __launch_bounds__(256, 2) void k_gemm_narrow(GemmArgs g)
 {
     extern __shared__ __align__(1024) unsigned char narrow_lds[];
-    constexpr int E = kChunk<T>, kRow = KS * 4;        // chunks in a row of B
-    lds_byte *lds = (lds_byte *)narrow_lds;
+    constexpr int E = kChunk<T>, kRow = KS * 4;        // chunks in a row of A or B
+    constexpr int MT = narrow_tiles(KS), kRows = 64 * MT, kLoads = kRows * kRow / 256, kStep = 256 / kRow;
+    lds_byte *strip_lds = (lds_byte *)narrow_lds, *lds = strip_lds + narrow_strip_bytes(KS);
     const int pairs = (g.n + 31) / 32, n_pad = pairs * 32;
     // the first element of chunk c, and how many of its elements are not its own
     auto start = [&](int c) { return FULL || c * E <= g.k - E ? c * E : g.k - E; };
@@ -533,57 +537,78 @@ __global__ __launch_bounds__(256, KS <= 8 ? 4 : 2) void k_gemm_narrow(GemmArgs g
         __builtin_memcpy(&f, e, 16);
         *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
     }
-    __syncthreads();
     const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
-    const int strips = (g.m + 15) / 16, step = gridDim.x * 4;
-    auto fetch = [&](int strip, Fragment (&f)[KS]) {
-        const int m = strip * 16 + j;           // rows beyond the last repeat it; they are not stored
-        const T *p = static_cast<const T *>(g.a) + (m < g.m ? m : g.m - 1) * g.lda;
+    const int row0 = (wave_base() >> 6) * 16 * MT;       // this wave's rows of a strip
+    const int strips = (int)(((int64_t)g.m + kRows - 1) / kRows);
+    // this thread's chunk of a row, and its rows of a strip
+    const int my_chunk = threadIdx.x % kRow, my_row = threadIdx.x / kRow;
+    const int my_start = start(my_chunk), my_extra = extra(my_chunk);
+    Vec<T, E> next[kLoads];
+    auto fetch = [&](int strip) {
 #pragma unroll
-        for (int s = 0; s < KS; s++) {
-            const Vec<T, E> v = load_vec<T, E>(p + start(4 * s + c));
-            __builtin_memcpy(&f[s], &v, 16);
+        for (int i = 0; i < kLoads; i++) {
+            const int m = strip * kRows + my_row + i * kStep;       // (rows beyond the last repeat it)
+            next[i] = load_vec<T, E>(static_cast<const T *>(g.a) + (m < g.m ? m : g.m - 1) * g.lda + my_start);
         }
     };
-    auto mask = [&](Fragment &f, int skip) {
-#pragma unroll
-        for (int d = 0; d < 4; d++) {
-            if constexpr (sizeof(T) == 4)
-                f.u[d] = d >= skip ? f.u[d] : 0u;
-            else
-                f.u[d] &= (2 * d >= skip ? 0xffffu : 0u) | (2 * d + 1 >= skip ? 0xffff0000u : 0u);
-        }
-    };
-    Fragment next[KS];
-    int strip = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (strip < strips) fetch(strip, next);
+    int strip = blockIdx.x;
+    if (strip < strips) fetch(strip);
     const int row = 8 * (j >> 2) + (j & 3);
-    for (; strip < strips; strip += step) {
-        Fragment fa[KS];
+    for (; strip < strips; strip += gridDim.x) {
 #pragma unroll
-        for (int s = 0; s < KS; s++) {
-            fa[s] = next[s];
-            if constexpr (!FULL) mask(fa[s], extra(4 * s + c));
+        for (int i = 0; i < kLoads; i++) {
+            const int r = my_row + i * kStep;
+            Fragment f;
+            __builtin_memcpy(&f, &next[i], 16);
+            if constexpr (!FULL) {
+#pragma unroll
+                for (int d = 0; d < 4; d++) {
+                    if constexpr (sizeof(T) == 4)
+                        f.u[d] = d >= my_extra ? f.u[d] : 0u;
+                    else
+                        f.u[d] &= (2 * d >= my_extra ? 0xffffu : 0u) | (2 * d + 1 >= my_extra ? 0xffff0000u : 0u);
+                }
+            }
+            *(__attribute__((address_space(3))) u32x4 *)(strip_lds + (r * kRow + (my_chunk ^ (r & 7))) * 16) = f.u;
         }
-        if (strip + step < strips) fetch(strip + step, next);
-        const int m = strip * 16 + j;
+        wait_for_lds<false>();
+        meet();
+        if (strip + (int)gridDim.x < strips) fetch(strip + gridDim.x);
+        Fragment fa[MT][KS];
+#pragma unroll
+        for (int t = 0; t < MT; t++)
+#pragma unroll
+            for (int s = 0; s < KS; s++) {
+                const int r = row0 + 16 * t + j;
+                fa[t][s].u = *(const __attribute__((address_space(3))) u32x4 *)(
+                    strip_lds + (r * kRow + ((4 * s + c) ^ (r & 7))) * 16);
+            }
+        wait_for_lds<false>();
+        meet();
         for (int p = 0; p < pairs; p++) {
-            f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+            f32x4 acc[MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; t++) acc[t][0] = acc[t][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = 0; s < KS; s++)
 #pragma unroll
-                for (int t = 0; t < 2; t++) {
-                    const int n = 32 * p + row + 4 * t;
+                for (int h = 0; h < 2; h++) {
+                    const int n = 32 * p + row + 4 * h;
                     Fragment fb;
                     fb.u = *(const __attribute__((address_space(3))) u32x4 *)(
                         lds + (n * kRow + ((4 * s + c) ^ narrow_swizzle(n))) * 16);
-                    acc[t] = mma<T>(fb, fa[s], acc[t]);
+#pragma unroll
+                    for (int t = 0; t < MT; t++) acc[t][h] = mma<T>(fb, fa[t][s], acc[t][h]);
                 }
             const int n = 32 * p + 8 * c;
-            if (m < g.m && n < g.n) {
-                float v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3],
-                              acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
-                finish<ACT, T, 8>(g, m, n, v);
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                const int m = strip * kRows + row0 + 16 * t + j;
+                if (m < g.m && n < g.n) {
+                    float v[8] = {acc[t][0][0], acc[t][0][1], acc[t][0][2], acc[t][0][3],
+                                  acc[t][1][0], acc[t][1][1], acc[t][1][2], acc[t][1][3]};
+                    finish<ACT, T, 8>(g, m, n, v);
+                }
             }
         }
     }
@@ -663,6 +688,202 @@ __global__ __launch_bounds__(1024) void k_column_join(GradArgs g)
         s = 0.0;
         for (int w = 0; w < 16; w++) s += lds[w][at];
         g.sums[n] = (float)s;
+    }
+}
+
+// The whole gradient of a narrow product in one pass over its rows: x, dy and
+// preact are read once and dx is written, which is all the memory it needs (the
+// three products apart read x and dz again and write dz).  A workgroup of eight
+// waves takes strips of 64 rows: it forms dz in registers (and its column sums,
+// unrounded), writes dz, rounded, and x to LDS, and from there
+//   dx = dz w      each wave for its 16 KT columns of dx, w in registers;
+//   dw += dz^T x   each wave for the same columns, all n, over the strip's rows
+//                  read back transposed; summed in registers to the end.
+// The next strip's loads are in flight meanwhile, and the LDS tiles are
+// double, so the waves meet once a strip.
+//
+// LDS rows of 16-byte chunks, chunk c of row r at c ^ f(r) (rows of 128 bytes)
+// or c ^ 2 f(r): f differs over eight rows in a row and over the rows r .. r+3,
+// r+8 .. r+11 that half a transposing read's lanes name.
+constexpr int kStripRows = 64, kNarrowThreads = 512;
+__device__ __forceinline__ int strip_swizzle(int row, int chunks)
+{
+    const int f = (row & 3) | (((row >> 3) ^ (row >> 2)) & 1) << 2;
+    return chunks == 8 ? f : 2 * f;
+}
+
+template <typename T, int NT, int KT, int ACT>
+__global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(NarrowGradArgs a)
+{
+    constexpr int kZChunks = NT * 2, kXChunks = KT * 16;                  // chunks of an LDS row
+    constexpr int kZBytes = kStripRows * kZChunks * 16, kXBytes = kStripRows * kXChunks * 16;
+    constexpr int kZLoads = kStripRows * kZChunks / kNarrowThreads, kXLoads = kStripRows * kXChunks / kNarrowThreads;
+    constexpr int NS = NT / 2;                                            // fragments of n
+    static_assert(sizeof(T) == 2 && kZLoads >= 1, "");
+    __shared__ __align__(1024) unsigned char smem[2 * (kZBytes + kXBytes)];
+    lds_byte *lds = (lds_byte *)smem;
+    const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const int k_wave = (wave_base() >> 6) * 16 * KT;
+    const int strips = (a.rows + kStripRows - 1) / kStripRows;
+    // w as the first operand, k along the fragment's rows (in the order that
+    // leaves a lane 8 neighbouring k where KT is even), n along the reduction
+    Fragment fw[KT][NS];
+    auto k_of = [&](int kt, int row) {
+        return KT % 2 == 0 ? k_wave + 32 * (kt >> 1) + 8 * (row >> 2) + 4 * (kt & 1) + (row & 3) : k_wave + 16 * kt + row;
+    };
+#pragma unroll
+    for (int kt = 0; kt < KT; kt++)
+#pragma unroll
+        for (int s = 0; s < NS; s++) {
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int n = 32 * s + 8 * c + i, k = k_of(kt, j);
+                e[i] = a.dx && n < a.n && k < a.k ? static_cast<const T *>(a.w)[n * a.ldw + k] : (T)0.0f;
+            }
+            __builtin_memcpy(&fw[kt][s], e, 16);
+        }
+    // this thread's chunks of a strip: their rows and columns
+    const int z_col = threadIdx.x % kZChunks * 8, z_row = threadIdx.x / kZChunks;
+    const int x_col = threadIdx.x % kXChunks * 8, x_row = threadIdx.x / kXChunks;
+    constexpr int kZStep = kNarrowThreads / kZChunks, kXStep = kNarrowThreads / kXChunks;
+    const bool z_on = z_col < a.n, x_on = x_col < a.k && a.dw;
+    Vec<T, 8> vd[kZLoads], vz[kZLoads], vx[kXLoads];
+    auto fetch = [&](int strip) {
+        // rows and columns that are not there repeat others, and are set to 0 later
+        const int r0 = strip * kStripRows;
+#pragma unroll
+        for (int i = 0; i < kZLoads; i++) {
+            const int r = r0 + z_row + i * kZStep, rr = r < a.rows ? r : a.rows - 1, cc = z_on ? z_col : 0;
+            vd[i] = load_vec<T, 8>(static_cast<const T *>(a.dy) + rr * a.ldd + cc);
+            if (ACT != CPE_ACT_NONE) vz[i] = load_vec<T, 8>(static_cast<const T *>(a.preact) + rr * a.ldp + cc);
+        }
+        if (!a.dw) return;
+#pragma unroll
+        for (int i = 0; i < kXLoads; i++) {
+            const int r = r0 + x_row + i * kXStep, rr = r < a.rows ? r : a.rows - 1;
+            vx[i] = load_vec<T, 8>(static_cast<const T *>(a.x) + rr * a.ldx + (x_on ? x_col : 0));
+        }
+    };
+    f32x4 acc[NT][KT];
+    float sums[8];
+#pragma unroll
+    for (int n = 0; n < NT; n++)
+#pragma unroll
+        for (int k = 0; k < KT; k++) acc[n][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 8; i++) sums[i] = 0.0f;
+    int strip = blockIdx.x, turn = 0;
+    if (strip < strips) fetch(strip);
+    for (; strip < strips; strip += gridDim.x, turn ^= 1) {
+        lds_byte *lz = lds + turn * (kZBytes + kXBytes), *lx = lz + kZBytes;
+        const int r0 = strip * kStripRows;
+#pragma unroll
+        for (int i = 0; i < kZLoads; i++) {
+            const int r = z_row + i * kZStep;
+            const bool on = z_on && r0 + r < a.rows;
+            T e[8];
+#pragma unroll
+            for (int v = 0; v < 8; v++) {
+                float dz = (float)vd[i].v[v];
+                if constexpr (ACT != CPE_ACT_NONE) dz *= activate_grad<ACT>((float)vz[i].v[v]);
+                dz = on ? dz : 0.0f;
+                sums[v] += dz;
+                e[v] = (T)dz;
+            }
+            Fragment f;
+            __builtin_memcpy(&f, e, 16);
+            *(__attribute__((address_space(3))) u32x4 *)(
+                lz + (r * kZChunks + ((z_col >> 3) ^ strip_swizzle(r, kZChunks))) * 16) = f.u;
+        }
+        if (a.dw) {
+#pragma unroll
+            for (int i = 0; i < kXLoads; i++) {
+                const int r = x_row + i * kXStep;
+                Fragment f;
+                __builtin_memcpy(&f, &vx[i], 16);
+                if (!x_on || r0 + r >= a.rows) f.u = u32x4{0, 0, 0, 0};
+                *(__attribute__((address_space(3))) u32x4 *)(
+                    lx + (r * kXChunks + ((x_col >> 3) ^ strip_swizzle(r, kXChunks))) * 16) = f.u;
+            }
+        }
+        wait_for_lds<false>();
+        meet();
+        if (strip + (int)gridDim.x < strips) fetch(strip + gridDim.x);
+        if (a.dw && k_wave < a.k) {
+            // the fragment of sixteen columns from `col` on over rows 32 s .. 32 s + 31, transposed
+            auto column = [&](const lds_byte *tile, int chunks, int col, int s) {
+                Fragment f;
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    const int r = 32 * s + 8 * c + 4 * t + (j >> 2), chunk = (col >> 3) + ((j & 3) >> 1);
+                    f.s[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(
+                        tile + (r * chunks + (chunk ^ strip_swizzle(r, chunks))) * 16 + (j & 1) * 8));
+                }
+                return f;
+            };
+#pragma unroll
+            for (int s = 0; s < kStripRows / 32; s++) {
+                Fragment fz[NT], fx[KT];
+#pragma unroll
+                for (int k = 0; k < KT; k++) fx[k] = column(lx, kXChunks, k_wave + 16 * k, s);
+#pragma unroll
+                for (int n = 0; n < NT; n++) fz[n] = column(lz, kZChunks, 16 * n, s);
+#pragma unroll
+                for (int n = 0; n < NT; n++)
+#pragma unroll
+                    for (int k = 0; k < KT; k++) acc[n][k] = mma<T>(fx[k], fz[n], acc[n][k]);
+            }
+        }
+        if (a.dx && k_wave < a.k) {
+#pragma unroll
+            for (int t = 0; t < kStripRows / 16; t++) {
+                const int r = 16 * t + j;
+                Fragment fz[NS];
+#pragma unroll
+                for (int s = 0; s < NS; s++)
+                    fz[s].u = *(const __attribute__((address_space(3))) u32x4 *)(
+                        lz + (r * kZChunks + ((4 * s + c) ^ strip_swizzle(r, kZChunks))) * 16);
+                constexpr int P = KT % 2 == 0 ? 2 : 1;
+#pragma unroll
+                for (int kt = 0; kt < KT; kt += P) {
+                    Vec<T, 4 * P> o;
+#pragma unroll
+                    for (int h = 0; h < P; h++) {
+                        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int s = 0; s < NS; s++) v = mma<T>(fw[kt + h][s], fz[s], v);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) o.v[4 * h + i] = (T)v[i];
+                    }
+                    const int k = k_of(kt, 4 * c);
+                    if (r0 + r < a.rows && k < a.k)
+                        store_vec<T, 4 * P>(static_cast<T *>(a.dx) + (r0 + r) * a.lddx + k, o);
+                }
+            }
+        }
+    }
+    if (a.dw) {
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+            for (int k = 0; k < KT; k++) {
+                const int nn = 16 * n + j, kk = k_wave + 16 * k + 4 * c;
+                if (nn < a.n && kk < a.k)
+                    *reinterpret_cast<f32x4 *>(a.part + ((int64_t)blockIdx.x * a.n + nn) * a.k + kk) = acc[n][k];
+            }
+    }
+    if (a.dbias) {
+        float *row = reinterpret_cast<float *>(smem);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; i++) row[z_row * (kZChunks * 8) + z_col + i] = sums[i];
+        __syncthreads();
+        if ((int)threadIdx.x < a.n) {
+            float s = 0.0f;
+            for (int r = 0; r < kZStep; r++) s += row[r * (kZChunks * 8) + threadIdx.x];
+            a.part_sums[(int64_t)blockIdx.x * a.n + threadIdx.x] = s;
+        }
     }
 }
 
@@ -759,9 +980,10 @@ template <typename T, bool B_ACROSS, int ACT>
 hipError_t launch_narrow(const GemmArgs &g, hipStream_t stream)
 {
     // as many workgroups as run at once, by LDS and registers
-    const int bytes = narrow_bytes<T>(g), by_lds = (160 << 10) / bytes, by_regs = narrow_steps<T>(g.k) <= 8 ? 4 : 2;
-    const int64_t want = ceil_div(ceil_div(g.m, 16), 4), most = 256 * (by_lds < by_regs ? by_lds : by_regs);
-    const dim3 grid((unsigned)(want < most ? want : most));
+    const int ks = narrow_steps<T>(g.k), bytes = narrow_bytes<T>(g) + narrow_strip_bytes(ks);
+    const int64_t strips = ceil_div(g.m, 64 * narrow_tiles(ks)), by_lds = (160 << 10) / bytes;
+    const int64_t most = 256 * (by_lds < 2 ? by_lds : 2);
+    const dim3 grid((unsigned)(strips < most ? strips : most));
     auto launch = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
         if (g.k == KS * kNarrowStep<T>)
@@ -843,6 +1065,71 @@ hipError_t launch_grad_type(const GradArgs &g, hipStream_t stream)
     if (g.n % 4 == 0) return launch_grad_width<T, 4>(g, stream);
     if (g.n % 2 == 0) return launch_grad_width<T, 2>(g, stream);
     return launch_grad_width<T, 1>(g, stream);
+}
+
+// dw and dbias over the workgroups' partials, four values per 16 lanes.
+template <typename T>
+__global__ __launch_bounds__(256) void k_narrow_grad_join(NarrowGradArgs a)
+{
+    __shared__ f32x4 lds[16][16];
+    const int at = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    const int64_t of_dw = a.dw ? (int64_t)a.n * (a.k / 4) : 0, all = of_dw + (a.dbias ? a.n / 4 : 0);
+    const int64_t q = (int64_t)blockIdx.x * 16 + at;
+    const bool is_dw = q < of_dw;
+    const float *p = is_dw ? a.part + q * 4 : a.part_sums + (q - of_dw) * 4;
+    const int64_t step = is_dw ? (int64_t)a.n * a.k : a.n;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (q < all) {
+#pragma unroll 8
+        for (int s = lane; s < a.blocks; s += 16) v += *reinterpret_cast<const f32x4 *>(p + s * step);
+    }
+    lds[lane][at] = v;
+    __syncthreads();
+    if (lane > 0 || q >= all) return;
+#pragma unroll
+    for (int l = 1; l < 16; l++) v += lds[l][at];
+    if (is_dw) {
+        const int quads = a.k / 4, n = (int)(q / quads), k = (int)(q - (int64_t)n * quads) * 4;
+        Vec<T, 4> o;
+#pragma unroll
+        for (int i = 0; i < 4; i++) o.v[i] = (T)v[i];
+        store_vec<T, 4>(static_cast<T *>(a.dw) + n * a.lddw + k, o);
+    } else {
+        *reinterpret_cast<Vec<float, 4> *>(a.dbias + (q - of_dw) * 4) = Vec<float, 4>{{v[0], v[1], v[2], v[3]}};
+    }
+}
+
+template <typename T, int NT, int KT>
+hipError_t launch_narrow_grad_size(const NarrowGradArgs &a, hipStream_t stream)
+{
+    const dim3 grid(a.blocks), block(kNarrowThreads);
+    switch (a.act) {
+    case CPE_ACT_RELU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_RELU>), grid, block, 0, stream, a); break;
+    case CPE_ACT_SILU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_SILU>), grid, block, 0, stream, a); break;
+    case CPE_ACT_GELU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_GELU>), grid, block, 0, stream, a); break;
+    default: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_NONE>), grid, block, 0, stream, a); break;
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_narrow_grad_type(NarrowGradArgs a, hipStream_t stream)
+{
+    // one workgroup per CU: a second one would double the partial dw
+    const int64_t strips = ceil_div(a.rows, kStripRows);
+    a.blocks = (int32_t)(strips < 256 ? strips : 256);
+    const bool wide_n = a.n > 64;
+    hipError_t e;
+    if (a.k <= 128)
+        e = wide_n ? launch_narrow_grad_size<T, 8, 1>(a, stream) : launch_narrow_grad_size<T, 4, 1>(a, stream);
+    else if (a.k <= 256)
+        e = wide_n ? launch_narrow_grad_size<T, 8, 2>(a, stream) : launch_narrow_grad_size<T, 4, 2>(a, stream);
+    else
+        e = launch_narrow_grad_size<T, 4, 4>(a, stream);
+    if (e != hipSuccess || (!a.dw && !a.dbias)) return e;
+    const int64_t quads = (a.dw ? (int64_t)a.n * (a.k / 4) : 0) + (a.dbias ? a.n / 4 : 0);
+    hipLaunchKernelGGL(k_narrow_grad_join<T>, dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
 }  // namespace

@@ -47,7 +47,19 @@ hipError_t launch_grad(const cpe_linear *h, const GradArgs &g, hipStream_t strea
                                  : launch_grad_bf16(g, stream);
 }
 
+// The gradient in one pass: whole vectors of features, a dw that eight waves'
+// registers hold, and rows enough for every workgroup to have some.
+constexpr int kNarrowGradRows = 4096;
+
 }  // namespace
+
+namespace cpe {
+bool narrow_grad_fits(const NarrowGradArgs &a)
+{
+    if (a.rows < kNarrowGradRows || a.n % 8 != 0 || a.k % 8 != 0) return false;
+    return (a.n <= 128 && a.k <= 256) || (a.n <= 64 && a.k <= 512);
+}
+}  // namespace cpe
 
 extern "C" {
 
@@ -143,6 +155,33 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
     }
     if (dw && !check_matrix(h, dw, dw_ld, h->in)) return CPE_ERR_INVALID_ARG;
     (void)hipGetLastError();
+    if (h->dtype != CPE_F32) {
+        NarrowGradArgs a{};
+        a.x = x;
+        a.ldx = x_ld;
+        a.w = w;
+        a.ldw = w_ld;
+        a.dy = dy;
+        a.ldd = dy_ld;
+        a.preact = preact;
+        a.ldp = preact_ld;
+        a.dx = dx;
+        a.lddx = dx_ld;
+        a.dw = dw;
+        a.lddw = dw_ld;
+        a.dbias = dbias;
+        a.part = reinterpret_cast<float *>(h->ws);
+        a.part_sums = reinterpret_cast<float *>(h->ws + h->sums_at);
+        a.rows = rows;
+        a.n = h->out;
+        a.k = h->in;
+        a.act = h->act;
+        if (narrow_grad_fits(a)) {
+            const hipError_t e = h->dtype == CPE_F16 ? launch_narrow_grad_f16(a, stream)
+                                                     : launch_narrow_grad_bf16(a, stream);
+            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
+        }
+    }
     const void *dz = dy;
     int64_t dz_ld = dy_ld;
     if (dbias || (act && rows > 0)) {

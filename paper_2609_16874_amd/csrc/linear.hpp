@@ -45,11 +45,27 @@ struct GradArgs {
     int act;
 };
 
+// A narrow product's whole gradient: dz = dy act'(preact), dx = dz w,
+// dw = dz^T x, dbias = column sums of dz; those whose pointer is not null.
+struct NarrowGradArgs {
+    const void *x, *w, *dy, *preact;
+    int64_t ldx, ldw, ldd, ldp, lddx, lddw;
+    void *dx, *dw;
+    float *dbias;
+    float *part, *part_sums;                  // scratch: [blocks][n][k], [blocks][n]
+    int32_t rows, n, k, blocks;
+    int act;
+};
+
 hipError_t launch_gemm_f32(const GemmArgs &g, hipStream_t stream);
 hipError_t launch_gemm_f16(const GemmArgs &g, hipStream_t stream);
 hipError_t launch_gemm_bf16(const GemmArgs &g, hipStream_t stream);
 hipError_t launch_grad_f32(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_f16(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_bf16(const GradArgs &g, hipStream_t stream);
+// whether the gradient is done in one pass (16-bit types), and that pass
+bool narrow_grad_fits(const NarrowGradArgs &a);
+hipError_t launch_narrow_grad_f16(NarrowGradArgs a, hipStream_t stream);
+hipError_t launch_narrow_grad_bf16(NarrowGradArgs a, hipStream_t stream);
 
 }  // namespace cpe

@@ -19,7 +19,7 @@ SHAPES = [
     (1, 1, 1, 0), (1, 64, 16, 0), (1, 1000, 33, 0), (3, 7, 5, 1), (16, 100, 65, 0), (17, 256, 64, 8),
     (64, 72, 40, 0), (65, 64, 128, 0), (128, 128, 128, 0), (129, 100, 65, 3), (200, 8, 4, 0), (300, 257, 131, 0),
     (257, 520, 136, 24), (1000, 64, 200, 0), (100, 4096, 96, 0), (90, 2049, 130, 0), (5000, 24, 8, 0),
-    (12345, 48, 40, 0),
+    (12345, 48, 40, 0), (4100, 256, 128, 0), (4097, 512, 64, 8), (6001, 200, 120, 0), (9000, 136, 16, 5), (5000, 304, 40, 0),
 ]
 
 
