@@ -1,19 +1,20 @@
 // k_norm.hpp -- group norm with an activation over channels-last maps, and
 // its gradient (private to the library; included once per element type).
 //
-// Three passes, for maps of any size (k_norm_stats, k_norm_merge,
-// k_norm_apply; the gradient alike): a thread owns V neighbouring channels (up
+// Two passes, for maps of any size (k_norm_stats, k_norm_apply; the gradient
+// alike): a thread owns V neighbouring channels (up
 // to 16 bytes of a row) and walks down the rows, so its channel constants stay
 // in registers; a workgroup of 256 covers R = 256 / (C / V) whole rows at a
 // time, or one row in several column steps where C / V > 256.  The workgroups
 // take chunks of R x kNormUnroll rows in turn, so that the chip reads one
-// region of memory at a time, and the last pass takes them in reverse, from
-// the end that the first pass has left in the caches.
+// region of memory at a time, and the second pass takes them in reverse, from
+// the end that the first pass has left in the caches.  The first pass's last
+// workgroup of a sample (by a counter in memory) joins the partial results.
 //
 // One pass, where a group fits the registers of a workgroup (k_norm_group,
 // k_norm_grad_group): one launch, the map read once.
 //
-// Statistics.  In three passes each thread sums (x - s) and (x - s)^2 with s
+// Statistics.  In two passes each thread sums (x - s) and (x - s)^2 with s
 // its first value of the channel, so a mean far from zero cancels nothing;
 // threads, then workgroups, are merged as (count, mean, sum of squares about
 // the mean),
@@ -39,15 +40,144 @@ __device__ __forceinline__ int valid_pixels(const NormArgs &a, int b)
     return v < 0 ? 0 : v > a.pixels ? a.pixels : v;
 }
 
-// Chunks of `chunk` rows that workgroup i of `blocks` takes, and its rows.
-__device__ __forceinline__ int64_t block_rows(int rows, int chunk, int blocks, int i)
+// The rows of each workgroup: chunks of `chunk` rows are dealt to `blocks`
+// workgroups in turn, and the last one may be partial.
+struct DealtRows {
+    int chunk, full, more, last, missing;
+    __device__ __forceinline__ DealtRows(int rows, int chunk_, int blocks) : chunk(chunk_)
+    {
+        const int chunks = (int)(((int64_t)rows + chunk - 1) / chunk);
+        full = chunks / blocks;
+        more = chunks - full * blocks;
+        last = chunks > 0 ? (chunks - 1) % blocks : -1;
+        missing = (int)((int64_t)chunks * chunk - rows);
+    }
+    __device__ __forceinline__ int64_t of(int i, int n = 1) const       // of workgroups i .. i+n-1
+    {
+        const int extra = more - i < 0 ? 0 : more - i < n ? more - i : n;
+        return ((int64_t)full * n + extra) * chunk - (last >= i && last < i + n ? missing : 0);
+    }
+};
+
+// Store to a map.  Maps that the caches cannot hold beside what the second pass
+// reads again are written PAST them: 106M values in 16 bits take 108 us instead
+// of 130, the gradient of 30M in 32 bits 117 instead of 136.
+typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
+template <bool PAST, typename T, int V>
+__device__ __forceinline__ void store_map(T *p, const Vec<T, V> &v)
 {
-    const int chunks = (int)(((int64_t)rows + chunk - 1) / chunk);
-    if (i >= chunks) return 0;
-    const int mine = (chunks - i + blocks - 1) / blocks;
-    const bool last = (chunks - 1 - i) % blocks == 0;      // the chunk that may be partial is this workgroup's
-    return (int64_t)mine * chunk - (last ? (int64_t)chunks * chunk - rows : 0);
+    if constexpr (PAST && sizeof(v) == 16) {
+        raw16 w;
+        __builtin_memcpy(&w, &v, 16);
+        __builtin_nontemporal_store(w, reinterpret_cast<raw16 *>(p));
+    } else {
+        store_vec<T, V>(p, v);
+    }
 }
+
+// Partial results that another workgroup, maybe on another XCD, reads in the
+// same launch: stored and loaded at the device's scope, which goes past the
+// XCD's own L2.  (Release and acquire fences would write back and drop that
+// whole L2 in every workgroup: 80 us more at 1024 of them.)
+__device__ __forceinline__ void share(float2 *p, float x, float y)
+{
+    uint64_t w;
+    const float2 v = make_float2(x, y);
+    __builtin_memcpy(&w, &v, 8);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 shared_value(const float2 *p)
+{
+    const uint64_t w =
+        __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float2 v;
+    __builtin_memcpy(&v, &w, 8);
+    return v;
+}
+
+// Whether this workgroup is the last of `expected` to count itself here, so
+// that all of them have shared their results: each waits for its own stores to
+// be done (all counters of s_waitcnt at 0) before.  The counter is 0 again
+// afterwards.
+__device__ __forceinline__ bool last_to_arrive(int32_t *counter, int expected)
+{
+    __shared__ int arrived;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        arrived = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived == expected - 1) *counter = 0;
+    }
+    __syncthreads();
+    return arrived == expected - 1;
+}
+
+// Sums over `count` <= kJoinWays rows of G shared pairs, in 64 bits and a fixed
+// order: add(k, pair, s0, s1) for each, then done(g, s0, s1).  `lds` holds
+// kNormThreads pairs of double.
+constexpr int kJoinWays = kNormJoinWays;
+template <typename Add, typename Done>
+__device__ __forceinline__ void join_rows(const float2 *rows, int count, int groups, double *lds, Add add, Done done)
+{
+    const int wide = groups < kNormThreads ? groups : kNormThreads;
+    const int deep = kNormThreads / wide < kJoinWays ? kNormThreads / wide : kJoinWays;
+    const int at = threadIdx.x % wide, row = threadIdx.x / wide;
+    for (int g0 = 0; g0 < groups; g0 += wide) {
+        const int g = g0 + at;
+        double s0 = 0.0, s1 = 0.0;
+        if (row < deep && g < groups) {
+#pragma unroll 4
+            for (int k = row; k < count; k += deep) add(k, shared_value(rows + (int64_t)k * groups + g), s0, s1);
+        }
+        __syncthreads();
+        lds[threadIdx.x] = s0;
+        lds[kNormThreads + threadIdx.x] = s1;
+        __syncthreads();
+        if (row == 0 && g < groups) {
+            for (int k = 1; k < deep; k++) {
+                s0 += lds[k * wide + at];
+                s1 += lds[kNormThreads + k * wide + at];
+            }
+            done(g, s0, s1);
+        }
+    }
+}
+
+// Join the pairs that a sample's workgroups have shared in part[block][G], as
+// a tree of kJoinWays: the last workgroup of each kJoinWays to arrive joins
+// their rows, and the last of those the joined ones.  add(first, n, pair, ..):
+// the pair of n workgroups from `first` on; between(n, ..) turns the sums of n
+// workgroups' pairs into one, done(g, ..) takes the whole sample's.
+template <typename Add, typename Between, typename Done>
+__device__ __forceinline__ void join_sample(const NormArgs &a, int b, int i, const float2 *part, double *lds, Add add,
+                                            Between between, Done done)
+{
+    const int teams = (a.blocks + kJoinWays - 1) / kJoinWays, team = i / kJoinWays, first = team * kJoinWays;
+    const int size = a.blocks - first < kJoinWays ? a.blocks - first : kJoinWays;
+    int32_t *counters = a.counters + (int64_t)b * kNormCounters;
+    if (!last_to_arrive(counters + 1 + team, size)) return;
+    const float2 *mine = part + (int64_t)first * a.groups;
+    auto add_block = [&](int k, float2 p, double &s0, double &s1) { add(first + k, 1, p, s0, s1); };
+    if (teams == 1) {
+        join_rows(mine, size, a.groups, lds, add_block, done);
+        return;
+    }
+    float2 *joined = reinterpret_cast<float2 *>(a.joined) + (int64_t)b * kJoinWays * a.groups;
+    join_rows(mine, size, a.groups, lds, add_block, [&](int g, double s0, double s1) {
+        const float2 p = between(first, size, s0, s1);
+        share(joined + team * a.groups + g, p.x, p.y);
+    });
+    if (!last_to_arrive(counters, teams)) return;
+    join_rows(joined, teams, a.groups, lds,
+              [&](int k, float2 p, double &s0, double &s1) {
+                  const int n = a.blocks - k * kJoinWays < kJoinWays ? a.blocks - k * kJoinWays : kJoinWays;
+                  add(k * kJoinWays, n, p, s0, s1);
+              },
+              done);
+}
+static_assert(kNormBlocks <= kJoinWays * kJoinWays && kNormCounters >= 1 + kJoinWays, "two levels join a sample");
 
 // c / cpg for c < 8192 through the reciprocal: c + 1/2 is at least 1/2 from a
 // multiple of cpg, and the product's error stays under 1e-3 / cpg.
@@ -136,14 +266,15 @@ __device__ __forceinline__ double sum_lanes(double v, int lanes)
 
 // Visit this workgroup's chunks of `rows` rows: body(r, count) with r this
 // thread's first row, of `count` rows cols.rows apart.  Chunk c goes to
-// workgroup c mod blocks; REVERSE takes them from the far end.
+// workgroup c mod blocks; REVERSE takes a workgroup's chunks from the last.
 template <bool REVERSE, int V, typename F>
 __device__ __forceinline__ void for_chunks(const Columns<V> &cols, int rows, int blocks, int i, F body)
 {
     const int chunk = cols.rows * kNormUnroll;
     const int chunks = (int)(((int64_t)rows + chunk - 1) / chunk);
+    const int64_t last = i + (int64_t)((chunks - 1 - i) / blocks) * blocks;
     for (int64_t c = i; c < chunks; c += blocks) {
-        const int64_t r = (REVERSE ? chunks - 1 - c : c) * chunk + cols.row;
+        const int64_t r = (REVERSE ? last - (c - i) : c) * chunk + cols.row;
         const int64_t left = (rows - r + cols.rows - 1) / cols.rows;
         body(r, r >= rows ? 0 : left < kNormUnroll ? (int)left : kNormUnroll);
     }
@@ -227,7 +358,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
     const int lanes = lanes_per_group(a.groups), upg = units / a.groups, entries = cols.rows * upg;
     const int lane = threadIdx.x & (lanes - 1);
     const float inv_upg = 1.0f / (float)upg;
-    const int64_t n_rows = block_rows(pb, cols.rows * kNormUnroll, a.blocks, i);
+    const DealtRows rows(pb, a.chunk, a.blocks);
+    const int64_t n_rows = rows.of(i);
     const float inv_n = 1.0f / ((float)(n_rows > 0 ? n_rows : 1) * (float)(upg * U));
     float2 *part = reinterpret_cast<float2 *>(a.part) + (int64_t)blockIdx.x * a.groups;
     for (int g0 = 0; g0 < a.groups; g0 += kNormThreads / lanes) {
@@ -245,59 +377,34 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
             if (n > 0.0f) m2 += fmaf(n * d, d, lm2[at]);
         }
         m2 = sum_lanes(m2, lanes);
-        if (on && lane == 0) part[g] = make_float2(mean, m2);
+        if (on && lane == 0) share(part + g, mean, m2);
     }
+    // s0 and s1: sums of n mean and of M2 + n mean^2
+    const double per_row = (double)(upg * U);
+    join_sample(
+        a, b, i, part - (int64_t)i * a.groups, reinterpret_cast<double *>(lds),
+        [&](int first, int count, float2 p, double &s0, double &s1) {
+            const double n = (double)rows.of(first, count) * per_row;
+            if (n > 0.0) {
+                s0 += n * (double)p.x;
+                s1 += (double)p.y + n * (double)p.x * (double)p.x;
+            }
+        },
+        [&](int first, int count, double s0, double s1) {
+            const double n = (double)rows.of(first, count) * per_row, m = n > 0.0 ? s0 / n : 0.0;
+            return make_float2((float)m, (float)(s1 - s0 * m));
+        },
+        [&](int g, double s0, double s1) {
+            const double n = pb > 0 ? (double)pb * per_row : 1.0;
+            const double mean = s0 / n, square = s1 / n - mean * mean, var = square < 0.0 ? 0.0 : square;
+            reinterpret_cast<float2 *>(a.stats)[(int64_t)b * a.groups + g] =
+                make_float2((float)mean, (float)(1.0 / sqrt(var + a.eps)));
+        });
 }
-
-// stats[b][g] = (mean, rstd) from the workgroups' partials: one workgroup per
-// group, its threads' at most kMergeEach partials in flight together.
-constexpr int kMergeEach = 8;
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_norm_merge(NormArgs a)
-{
-    __shared__ double lds[2][THREADS / 64];
-    const int b = blockIdx.x / a.groups, g = blockIdx.x - b * a.groups;
-    const int pb = valid_pixels(a, b), cpg = a.channels / a.groups;
-    const float2 *part = reinterpret_cast<const float2 *>(a.part) + (int64_t)b * a.blocks * a.groups + g;
-    float2 p[kMergeEach];
-    double rows[kMergeEach];
-#pragma unroll
-    for (int e = 0; e < kMergeEach; e++) {
-        const int i = threadIdx.x + e * THREADS;
-        const int64_t mine = i < a.blocks ? block_rows(pb, a.chunk, a.blocks, i) : 0;
-        p[e] = mine > 0 ? part[(int64_t)i * a.groups] : make_float2(0.0f, 0.0f);
-        rows[e] = (double)mine;
-    }
-    auto total = [&](double v, int slot) {
-        v = sum_lanes(v, 64);
-        if constexpr (THREADS == 64) return v;
-        if ((threadIdx.x & 63) == 0) lds[slot][threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0;
-        for (int w = 0; w < THREADS / 64; w++) v += lds[slot][w];
-        return v;
-    };
-    const double n = pb > 0 ? pb : 1;
-    double mean = 0.0, m2 = 0.0;
-#pragma unroll
-    for (int e = 0; e < kMergeEach; e++) mean += rows[e] * (double)p[e].x;
-    mean = total(mean, 0) / n;
-#pragma unroll
-    for (int e = 0; e < kMergeEach; e++) {
-        const double d = (double)p[e].x - mean;
-        if (rows[e] > 0.0) m2 += (double)p[e].y + rows[e] * cpg * d * d;
-    }
-    m2 = total(m2, 1);
-    if (threadIdx.x == 0) {
-        const double var = m2 > 0.0 || m2 != m2 ? m2 / (n * cpg) : 0.0;
-        reinterpret_cast<float2 *>(a.stats)[blockIdx.x] = make_float2((float)mean, (float)(1.0 / sqrt(var + a.eps)));
-    }
-}
-static_assert(kNormBlocks <= 256 * kMergeEach, "every partial of a group has a place");
 
 // y = act((x - mean) (rstd gamma) + beta); pixels from the sample's count on
 // are set to 0.
-template <typename T, int V, bool GROUPED, int ACT>
+template <typename T, int V, bool GROUPED, bool PAST, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 {
     const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
@@ -323,14 +430,14 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 #pragma unroll
                 for (int u = 0; u < kNormUnroll; u++) f[u] = load_vec<T, V>(px + u * xs);
 #pragma unroll
-                for (int u = 0; u < kNormUnroll; u++) store_vec<T, V>(py + u * ys, one(f[u]));
+                for (int u = 0; u < kNormUnroll; u++) store_map<PAST>(py + u * ys, one(f[u]));
             } else {
                 for (int u = 0; u < count; u++) {
                     Vec<T, V> o;
 #pragma unroll
                     for (int v = 0; v < V; v++) o.v[v] = (T)0.0f;
                     if (r + u * cols.rows < pb) o = one(load_vec<T, V>(px + u * xs));
-                    store_vec<T, V>(py + u * ys, o);
+                    store_map<PAST>(py + u * ys, o);
                 }
             }
         });
@@ -386,73 +493,80 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
         }
     }
     __syncthreads();
-    float2 *part = reinterpret_cast<float2 *>(a.part) + (int64_t)blockIdx.x * C;
     for (int c = threadIdx.x; c < C; c += kNormThreads) {
         float s1 = 0.0f, s2 = 0.0f;
         for (int r = 0; r < cols.rows; r++) {
             s1 += l1[r * C + c];
             s2 += l2[r * C + c];
         }
-        part[c] = make_float2(s1, s2);
+        if (a.dgamma || a.dbeta) reinterpret_cast<float2 *>(a.part)[(int64_t)blockIdx.x * C + c] = make_float2(s1, s2);
+        const float gamma = a.gamma ? a.gamma[c] : 1.0f;
+        l1[c] = s1 * gamma;     // (row 0, of which this thread has just read its place)
+        l2[c] = s2 * gamma;
     }
+    __syncthreads();
+    if (!a.out) return;
+    const int lanes = lanes_per_group(a.groups), cpg = C / a.groups, lane = threadIdx.x & (lanes - 1);
+    float2 *part = reinterpret_cast<float2 *>(a.group_part) + (int64_t)blockIdx.x * a.groups;
+    for (int g0 = 0; g0 < a.groups; g0 += kNormThreads / lanes) {
+        const int g = g0 + threadIdx.x / lanes;
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int e = lane; g < a.groups && e < cpg; e += lanes) {
+            s1 += l1[g * cpg + e];
+            s2 += l2[g * cpg + e];
+        }
+        s1 = sum_lanes(s1, lanes);
+        s2 = sum_lanes(s2, lanes);
+        if (g < a.groups && lane == 0) share(part + g, s1, s2);
+    }
+    join_sample(
+        a, b, i, part - (int64_t)i * a.groups, reinterpret_cast<double *>(lds),
+        [](int, int, float2 p, double &s1, double &s2) {
+            s1 += (double)p.x;
+            s2 += (double)p.y;
+        },
+        [](int, int, double s1, double s2) { return make_float2((float)s1, (float)s2); },
+        [&](int g, double s1, double s2) {
+            const double n = pb > 0 ? (double)pb * cpg : 1.0;
+            reinterpret_cast<float2 *>(a.group_sums)[(int64_t)b * a.groups + g] =
+                make_float2((float)(s1 / n), (float)(s2 / n));
+        });
 }
 
-// chan[b][c] = the workgroups' partials summed: kMergeChannels channels of a
-// sample (a cache line of partials) per workgroup, 64 lanes of partials each.
-constexpr int kMergeChannels = 16, kMergeLanes = 64;
-__global__ __launch_bounds__(kMergeChannels *kMergeLanes) void k_norm_grad_merge(NormArgs a)
+// dgamma and dbeta of kVectorChannels channels (a cache line of partials) as
+// sums over `partials` of them, by a workgroup of kNormThreads.
+constexpr int kVectorChannels = 16;
+__device__ __forceinline__ void sum_vectors(const NormArgs &a, int slab, int64_t partials)
 {
-    __shared__ double l1[kMergeLanes / 4][kMergeChannels], l2[kMergeLanes / 4][kMergeChannels];
-    const int slabs = (a.channels + kMergeChannels - 1) / kMergeChannels;
-    const int b = blockIdx.x / slabs, at = threadIdx.x % kMergeChannels, lane = threadIdx.x / kMergeChannels;
-    const int c = (blockIdx.x - b * slabs) * kMergeChannels + at;
-    const float2 *part = reinterpret_cast<const float2 *>(a.part) + (int64_t)b * a.blocks * a.channels;
+    constexpr int kLanes = kNormThreads / kVectorChannels;
+    __shared__ double l1[kLanes][kVectorChannels], l2[kLanes][kVectorChannels];
+    const int at = threadIdx.x % kVectorChannels, lane = threadIdx.x / kVectorChannels;
+    const int c = slab * kVectorChannels + at;
     double s1 = 0.0, s2 = 0.0;
     if (c < a.channels) {
-#pragma unroll 8
-        for (int i = lane; i < a.blocks; i += kMergeLanes) {
-            const float2 p = part[(int64_t)i * a.channels + c];
+        const float2 *part = reinterpret_cast<const float2 *>(a.part) + c;
+#pragma unroll 16
+        for (int64_t i = lane; i < partials; i += kLanes) {
+            const float2 p = part[i * a.channels];
             s1 += (double)p.x;
             s2 += (double)p.y;
         }
     }
-    // a wave holds four lanes of partials, sixteen threads apart
-    s1 += __shfl_xor(s1, 16);
-    s2 += __shfl_xor(s2, 16);
-    s1 += __shfl_xor(s1, 32);
-    s2 += __shfl_xor(s2, 32);
-    if ((threadIdx.x & 63) < kMergeChannels) {
-        l1[threadIdx.x >> 6][at] = s1;
-        l2[threadIdx.x >> 6][at] = s2;
-    }
+    l1[lane][at] = s1;
+    l2[lane][at] = s2;
     __syncthreads();
-    if (threadIdx.x < kMergeChannels && c < a.channels) {
-        for (int w = 1; w < kMergeLanes / 4; w++) {
-            s1 += l1[w][at];
-            s2 += l2[w][at];
-        }
-        reinterpret_cast<float2 *>(a.chan)[(int64_t)b * a.channels + c] = make_float2((float)s1, (float)s2);
-    }
-}
-
-// dgamma and dbeta of channel c: sums over the samples.
-__device__ __forceinline__ void sum_samples(const NormArgs &a, int64_t c)
-{
-    if (c >= a.channels) return;
-    const float2 *chan = reinterpret_cast<const float2 *>(a.chan) + c;
-    double s1 = 0.0, s2 = 0.0;
-#pragma unroll 4
-    for (int b = 0; b < a.samples; b++) {
-        const float2 p = chan[(int64_t)b * a.channels];
-        s1 += (double)p.x;
-        s2 += (double)p.y;
+    if (lane > 0 || c >= a.channels) return;
+    for (int l = 1; l < kLanes; l++) {
+        s1 += l1[l][at];
+        s2 += l2[l][at];
     }
     if (a.dbeta) a.dbeta[c] = (float)s1;
     if (a.dgamma) a.dgamma[c] = (float)s2;
 }
-__global__ __launch_bounds__(64) void k_norm_grad_vectors(NormArgs a)
+template <int UNUSED>
+__global__ __launch_bounds__(kNormThreads) void k_norm_grad_vectors(NormArgs a)
 {
-    sum_samples(a, (int64_t)blockIdx.x * 64 + threadIdx.x);
+    sum_vectors(a, blockIdx.x, (int64_t)a.samples * a.blocks);
 }
 
 // One element of dx = du (rstd gamma) - rstd a/n - (x - mean) rstd^2 q/n, with
@@ -466,48 +580,28 @@ __device__ __forceinline__ float grad_one(const Channels<V, GROUPED> &ch, int v,
     return fmaf(du, ch.scale[v], fmaf(d, slope, flat));
 }
 
-// dx, and (the first workgroups) dgamma and dbeta.
-template <typename T, int V, bool GROUPED, int ACT>
-__global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a)
+// dx, and (the first `vectors` workgroups) dgamma and dbeta.
+template <typename T, int V, bool GROUPED, bool PAST, int ACT>
+__global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a, int vectors)
 {
-    extern __shared__ float lds[];      // [G][2]: the group's a / n and q / n
-    const int C = a.channels, cpg = C / a.groups;
-    const float2 *chan = reinterpret_cast<const float2 *>(a.chan);
-    if (a.dgamma || a.dbeta) sum_samples(a, (int64_t)blockIdx.x * kNormThreads + threadIdx.x);
-    const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
-    if (!a.out || b >= a.samples) return;
-    const int pb = valid_pixels(a, b);
-    const float inv_n = pb > 0 ? 1.0f / ((float)pb * (float)cpg) : 0.0f;
-    const int lanes = lanes_per_group(a.groups), lane = threadIdx.x & (lanes - 1);
-    for (int g0 = 0; g0 < a.groups; g0 += kNormThreads / lanes) {
-        const int g = g0 + threadIdx.x / lanes;
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int e = lane; g < a.groups && e < cpg; e += lanes) {
-            const int c = g * cpg + e;
-            const float2 p = chan[(int64_t)b * C + c];
-            const float gamma = a.gamma ? a.gamma[c] : 1.0f;
-            s1 = fmaf(gamma, p.x, s1);
-            s2 = fmaf(gamma, p.y, s2);
-        }
-        s1 = sum_lanes(s1, lanes);
-        s2 = sum_lanes(s2, lanes);
-        if (g < a.groups && lane == 0) {
-            lds[2 * g] = s1 * inv_n;
-            lds[2 * g + 1] = s2 * inv_n;
-        }
+    if ((int)blockIdx.x < vectors) {
+        sum_vectors(a, blockIdx.x, (int64_t)a.samples * a.blocks);
+        return;
     }
-    __syncthreads();
-    const Columns<V> cols(C);
-    const float inv_cpg = 1.0f / (float)cpg;
+    const int w = blockIdx.x - vectors, b = w / a.blocks, i = w - b * a.blocks;
+    const int pb = valid_pixels(a, b);
+    const Columns<V> cols(a.channels);
+    const float inv_cpg = 1.0f / (float)(a.channels / a.groups);
+    const float2 *sums = reinterpret_cast<const float2 *>(a.group_sums) + (int64_t)b * a.groups;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
         const Channels<V, GROUPED> ch(a, b, col);
         constexpr int N = GROUPED ? 1 : V;
         float flat[N], slope[N];
 #pragma unroll
         for (int v = 0; v < N; v++) {
-            const int g = group_of(col * V + v, inv_cpg);
-            flat[v] = -ch.rstd(v) * lds[2 * g];
-            slope[v] = -ch.rstd(v) * ch.rstd(v) * lds[2 * g + 1];
+            const float2 aq = sums[group_of(col * V + v, inv_cpg)];       // a / n and q / n
+            flat[v] = -ch.rstd(v) * aq.x;
+            slope[v] = -ch.rstd(v) * ch.rstd(v) * aq.y;
         }
         auto one = [&](const Vec<T, V> &fx, const Vec<T, V> &fd) {
             Vec<T, V> o;
@@ -532,14 +626,14 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a)
                     fd[u] = load_vec<T, V>(pd + u * ds);
                 }
 #pragma unroll
-                for (int u = 0; u < kNormUnroll; u++) store_vec<T, V>(po + u * os, one(fx[u], fd[u]));
+                for (int u = 0; u < kNormUnroll; u++) store_map<PAST>(po + u * os, one(fx[u], fd[u]));
             } else {
                 for (int u = 0; u < count; u++) {
                     Vec<T, V> o;
 #pragma unroll
                     for (int v = 0; v < V; v++) o.v[v] = (T)0.0f;
                     if (r + u * cols.rows < pb) o = one(load_vec<T, V>(px + u * xs), load_vec<T, V>(pd + u * ds));
-                    store_vec<T, V>(po + u * os, o);
+                    store_map<PAST>(po + u * os, o);
                 }
             }
         });
@@ -731,7 +825,7 @@ __global__ __launch_bounds__(kGroupThreads) void k_norm_grad_group(NormArgs a)
     for (int k = threadIdx.x; k < cpg; k += kGroupThreads) {
         const int64_t ch_at = at.g * cpg + k;
         if (a.samples > 1) {
-            reinterpret_cast<float2 *>(a.chan)[(int64_t)at.b * a.channels + ch_at] =
+            reinterpret_cast<float2 *>(a.part)[(int64_t)at.b * a.channels + ch_at] =
                 make_float2(total[k], total[cpg + k]);
         } else {
             if (a.dbeta) a.dbeta[ch_at] = total[k];
@@ -765,45 +859,54 @@ int blocks_per_sample(const NormArgs &a)
     return (int)(want < cap ? want : cap < 1 ? 1 : cap);
 }
 
+// Whether every vector of the written map is 16-byte aligned (the stores past
+// the caches say so).
+template <typename T>
+bool aligned_rows(const NormArgs &a)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    return aligned_to(a.out, 16) && a.out_ld % E == 0 && (a.samples == 1 || a.out_sample % E == 0);
+}
+
 template <typename T, int V, bool GROUPED, int ACT>
 hipError_t launch_norm(NormArgs a, hipStream_t stream)
 {
     const int rows = a.channels / V >= kNormThreads ? 1 : kNormThreads / (a.channels / V);
-    const size_t lds = 2 * sizeof(float) * (size_t)rows * a.channels;
+    const size_t least = 2 * sizeof(double) * kNormThreads;       // (the join's)
+    const size_t whole = 2 * sizeof(float) * (size_t)rows * a.channels, units = GROUPED ? whole / V : whole;
+    const size_t lds = a.backward ? whole : units;
     a.chunk = rows * kNormUnroll;
+    a.blocks = a.samples > 0 ? blocks_per_sample(a) : 0;
+    const int64_t bytes = (int64_t)a.samples * a.pixels * a.channels * (int64_t)sizeof(T);
+    const bool past = V * sizeof(T) == 16 && bytes * (a.backward ? 3 : 2) > kCacheBytes && aligned_rows<T>(a);
+    const dim3 grid(a.samples * a.blocks), block(kNormThreads);
     if (!a.backward) {
-        a.blocks = blocks_per_sample(a);
-        hipLaunchKernelGGL((k_norm_stats<T, V, GROUPED>), dim3(a.samples * a.blocks), dim3(kNormThreads),
-                           GROUPED ? lds / V : lds, stream, a);
+        hipLaunchKernelGGL((k_norm_stats<T, V, GROUPED>), grid, block, lds > least ? lds : least, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if (a.blocks <= 64 * kMergeEach)
-            hipLaunchKernelGGL(k_norm_merge<64>, dim3(a.samples * a.groups), dim3(64), 0, stream, a);
+        if (past)
+            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, V * sizeof(T) == 16, ACT>), grid, block, 0, stream, a);
         else
-            hipLaunchKernelGGL(k_norm_merge<256>, dim3(a.samples * a.groups), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, false, ACT>), grid, block, 0, stream, a);
+        return hipGetLastError();
+    }
+    const int vectors = a.dgamma || a.dbeta ? (int)ceil_div(a.channels, kVectorChannels) : 0;
+    if (a.samples > 0) {
+        hipLaunchKernelGGL((k_norm_grad_sums<T, V, GROUPED, ACT>), grid, block, lds > least ? lds : least, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, ACT>), dim3(a.samples * a.blocks), dim3(kNormThreads), 0,
-                           stream, a);
-        return hipGetLastError();
     }
-    if (a.samples == 0) {
-        hipLaunchKernelGGL(k_norm_grad_vectors, dim3((unsigned)ceil_div(a.channels, 64)), dim3(64), 0, stream, a);
-        return hipGetLastError();
-    }
-    a.blocks = blocks_per_sample(a);
-    hipLaunchKernelGGL((k_norm_grad_sums<T, V, GROUPED, ACT>), dim3(a.samples * a.blocks), dim3(kNormThreads), lds,
-                       stream, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_norm_grad_merge, dim3(a.samples * (int)ceil_div(a.channels, kMergeChannels)),
-                       dim3(kMergeChannels * kMergeLanes), 0, stream, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const int vectors = (int)ceil_div(a.channels, kNormThreads), grid = a.samples * a.blocks;
-    hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, ACT>), dim3(grid > vectors ? grid : vectors),
-                       dim3(kNormThreads), 2 * sizeof(float) * a.groups, stream, a);
+    if (a.samples > 0 && a.out && past)
+        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, V * sizeof(T) == 16, ACT>), dim3(grid.x + vectors), block,
+                           0, stream, a, vectors);
+    else if (a.samples > 0 && a.out)
+        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, false, ACT>), dim3(grid.x + vectors), block, 0, stream, a,
+                           vectors);
+    else
+        hipLaunchKernelGGL(k_norm_grad_vectors<0>, dim3(vectors), block, 0, stream, a);
     return hipGetLastError();
 }
 
 // One pass where a group's values fit a workgroup's registers: 13 us against
-// 18 for three passes on small maps (calls as a program makes them), 21
+// 18 for more passes on small maps (calls as a program makes them), 21
 // against 29 at 16 x 1024 pixels x 32 groups of 32 channels in 16 bits.  Rows
 // of a group shorter than 32 bytes share their cache lines with other
 // workgroups, which costs more than the second reading on larger maps (16 x
@@ -833,7 +936,10 @@ hipError_t launch_group_held(const NormArgs &a, hipStream_t stream)
         hipLaunchKernelGGL((k_norm_grad_group<T, V, ACT, K>), grid, dim3(kGroupThreads), lds, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         if (a.samples == 1 || (!a.dgamma && !a.dbeta)) return hipSuccess;
-        hipLaunchKernelGGL(k_norm_grad_vectors, dim3((unsigned)ceil_div(a.channels, 64)), dim3(64), 0, stream, a);
+        NormArgs v = a;
+        v.blocks = 1;
+        hipLaunchKernelGGL(k_norm_grad_vectors<0>, dim3((unsigned)ceil_div(a.channels, kVectorChannels)),
+                           dim3(kNormThreads), 0, stream, v);
     }
     return hipGetLastError();
 }
@@ -856,7 +962,7 @@ hipError_t launch_norm_act(const NormArgs &a, hipStream_t stream)
         if (group_fits<T, 8>(a)) return launch_group<T, 8, ACT>(a, stream);
     if (group_fits<T, 4>(a)) return launch_group<T, 4, ACT>(a, stream);
     if (group_fits<T, 1>(a)) return launch_group<T, 1, ACT>(a, stream);
-    // three passes, in the widest vectors that divide a row
+    // two passes, in the widest vectors that divide a row
     if constexpr (sizeof(T) == 2) {
         if (cpg % 8 == 0) return launch_norm<T, 8, true, ACT>(a, stream);
         if (C % 8 == 0) return launch_norm<T, 8, false, ACT>(a, stream);

@@ -16,7 +16,7 @@ struct cpe_norm {
     float eps;
     int device;
     unsigned char *ws;
-    size_t ws_bytes, chan_at, stats_at;
+    size_t ws_bytes, group_part_at, group_sums_at, joined_at, counters_at, stats_at;
 };
 
 namespace {
@@ -64,7 +64,10 @@ NormArgs common_args(const cpe_norm *h, int32_t samples, int32_t pixels, const f
     a.beta = beta;
     a.valid = valid;
     a.part = reinterpret_cast<float *>(h->ws);
-    a.chan = reinterpret_cast<float *>(h->ws + h->chan_at);
+    a.group_part = reinterpret_cast<float *>(h->ws + h->group_part_at);
+    a.group_sums = reinterpret_cast<float *>(h->ws + h->group_sums_at);
+    a.joined = reinterpret_cast<float *>(h->ws + h->joined_at);
+    a.counters = reinterpret_cast<int32_t *>(h->ws + h->counters_at);
     a.samples = samples;
     a.pixels = pixels;
     a.channels = h->channels;
@@ -104,14 +107,26 @@ cpe_status cpe_norm_create(cpe_norm **out, int32_t max_samples, int32_t max_pixe
         return CPE_ERR_HIP;
     }
     const size_t blocks = max_samples > kNormBlocks ? max_samples : kNormBlocks;
-    h->chan_at = align256(blocks * channels * 8);
-    h->stats_at = h->chan_at + align256((size_t)max_samples * channels * 8);
-    h->ws_bytes = h->stats_at + align256((size_t)max_samples * groups * 8);
+    h->group_part_at = align256(blocks * channels * 8);
+    h->group_sums_at = h->group_part_at + align256(blocks * groups * 8);
+    h->stats_at = h->group_sums_at + align256((size_t)max_samples * groups * 8);
+    h->joined_at = h->stats_at + align256((size_t)max_samples * groups * 8);
+    // (only samples of more than kJoinWays workgroups join in two levels)
+    const size_t large = max_samples < kNormBlocks / kNormJoinWays ? max_samples : kNormBlocks / kNormJoinWays;
+    h->counters_at = h->joined_at + align256(large * kNormJoinWays * groups * 8);
+    h->ws_bytes = h->counters_at + align256((size_t)max_samples * kNormCounters * 4);
     void *p = nullptr;
     if (hipMalloc(&p, h->ws_bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete h;
         return CPE_ERR_OUT_OF_MEMORY;
+    }
+    if (hipMemset(static_cast<unsigned char *>(p) + h->counters_at, 0, h->ws_bytes - h->counters_at) != hipSuccess ||
+        hipDeviceSynchronize() != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipFree(p);
+        delete h;
+        return CPE_ERR_HIP;
     }
     h->ws = static_cast<unsigned char *>(p);
     *out = h;

@@ -10,8 +10,11 @@
 namespace cpe {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 2048;      // workgroups of a pass over the map (or one per sample)
+constexpr int kNormBlocks = 1024;      // workgroups of a pass over the map (or one per sample)
+constexpr int kNormJoinWays = 32;      // partial results that are joined at a time
+constexpr int kNormCounters = 64;      // per sample: of the join's teams and of the sample
 constexpr int kNormMaxChannels = 8192;
+constexpr int64_t kCacheBytes = (int64_t)128 << 20;      // read and written, half of what the last cache holds
 
 struct NormArgs {
     const void *x, *dy;
@@ -21,7 +24,10 @@ struct NormArgs {
     const int32_t *valid;               // may be null
     float *stats;                       // [samples][G][2]: written by the forward, read by the backward
     float *part;                        // scratch: [samples][blocks][G or C][2]
-    float *chan;                        // scratch: [samples][C][2] (backward)
+    float *group_part;                  // scratch (backward): [samples][blocks][G][2]
+    float *group_sums;                  // scratch (backward): [samples][G][2]
+    float *joined;                      // scratch: [samples][32][G][2], the first level of the join
+    int32_t *counters;                  // [samples][kNormCounters], 0 between calls
     float *dgamma, *dbeta;              // may be null
     int32_t samples, pixels, channels, groups;
     int32_t blocks, chunk;              // workgroups per sample, rows that each takes at a time
