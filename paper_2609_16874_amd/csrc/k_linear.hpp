@@ -91,7 +91,6 @@ struct Operand {
     static constexpr int E = kChunk<T>, R = kTile, kLoads = R * 8 / kGemmThreads;
     static constexpr int kPerRow = ACROSS ? R / E : 8;    // chunks in an LDS row
     static constexpr int kBytes = R * 128;
-    static constexpr int kReads = !ACROSS ? 1 : sizeof(T) == 4 ? 4 : 2;      // LDS reads of a fragment
     const T *base;          // DIRECT: of the workgroup; else of the first row
     int64_t step;
     uint32_t off[kLoads];   // DIRECT: bytes from the base
@@ -257,33 +256,13 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
-// The order of a half step: LDS reads, then loads, one between two matrix
-// instructions each, so that neither waits for the other's unit.
-template <int READS, int LOADS, int MULTIPLIES>
-__device__ __forceinline__ void interleave()
-{
-    constexpr int kMfma = 0x8, kVmem = 0x20, kLdsRead = 0x100;
-#pragma unroll
-    for (int i = 0; i < READS; i++) {
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 1, 0);
-        if (i < MULTIPLIES) __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-        __builtin_amdgcn_sched_group_barrier(kVmem, 1, 0);
-        if (READS + i < MULTIPLIES) __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    }
-    if constexpr (MULTIPLIES > READS + LOADS)
-        __builtin_amdgcn_sched_group_barrier(kMfma, MULTIPLIES - READS - LOADS, 0);
-}
-
 // Tiles of 128 x 128 outputs, a wave for each 64 x 64 of them, two LDS tiles of
 // kStepK k, two workgroups per CU.  A step's two halves of fragments alternate
 // in registers: the second half is read while the first is multiplied, then
 // the waves meet and read the next step's first half while the second is
 // multiplied.  At the meeting the next step's LDS tile has arrived (DIRECT: its
 // loads went straight to LDS) and every wave has read the present one, whose
-// place the loads of the step after next take from then on.
+// place the loads of the step after next take at once.
 //
 // The epilogue passes through LDS, a row's 16-byte chunks permuted by the
 // row, so that every row leaves as whole lines and the code that finishes a
@@ -350,40 +329,40 @@ __global__ __launch_bounds__(kGemmThreads, 2) void k_gemm(GemmArgs g)
 #pragma unroll
             for (int j = 0; j < W; j++) acc[i][j] = mma<T>(fb[half][j], fa[half][i], acc[i][j]);
     };
-    constexpr int kReads = W * (A::kReads + B::kReads), kMultiplies = W * W * (sizeof(T) == 4 ? 4 : 1);
+    // step t's first half of fragments is in flight; its LDS tile and (DIRECT) the
+    // next one's loads, or the next one's values in registers
     if (steps > 0) {
         fetch_any(0);
         commit(0);
         wait_for_lds<true>();
         meet();
+        if (steps > 1) fetch_any(1);
         read(0, 0);
     }
     int t = 0;
-    for (; t + 1 < whole; t++) {        // the steps whose loads are whole: no branch
+    for (; t + 2 < whole; t++) {        // the steps whose loads are whole: no branch
         wait_for_lds<false>();          // the fragments of the first half
         __builtin_amdgcn_sched_barrier(0);
-        fetch(std::false_type{}, t + 1);
         read(t, 1);
         multiply(0);
-        interleave<kReads, DIRECT ? A::kLoads + B::kLoads : 0, kMultiplies>();
         __builtin_amdgcn_sched_barrier(0);
         commit(t + 1);
         wait_for_lds<true>();
         meet();
         __builtin_amdgcn_sched_barrier(0);
+        fetch(std::false_type{}, t + 2);
         read(t + 1, 0);
         multiply(1);
-        interleave<kReads, 0, kMultiplies>();
         __builtin_amdgcn_sched_barrier(0);
     }
     for (; t < steps; t++) {
         const bool more = t + 1 < steps;
-        if (more) fetch_any(t + 1);
         read(t, 1);
         multiply(0);
         if (more) commit(t + 1);
         wait_for_lds<true>();
         meet();
+        if (t + 2 < steps) fetch_any(t + 2);
         if (more) read(t + 1, 0);
         multiply(1);
     }
