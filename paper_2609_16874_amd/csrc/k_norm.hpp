@@ -63,15 +63,26 @@ struct DealtRows {
 // reads again are written PAST them: 106M values in 16 bits take 108 us instead
 // of 130, the gradient of 30M in 32 bits 117 instead of 136.
 typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
-template <bool PAST, typename T, int V>
-__device__ __forceinline__ void store_map(T *p, const Vec<T, V> &v)
+template <bool PAST, int N, typename T, int V>
+__device__ __forceinline__ void store_map(T *p, int64_t step, const Vec<T, V> (&v)[N], int extra)
 {
-    if constexpr (PAST && sizeof(v) == 16) {
-        raw16 w;
-        __builtin_memcpy(&w, &v, 16);
-        __builtin_nontemporal_store(w, reinterpret_cast<raw16 *>(p));
-    } else {
-        store_vec<T, V>(p, v);
+    if (V > 1 && extra > 0) {       // all but the first `extra` values
+#pragma unroll
+        for (int u = 0; u < N; u++)
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (i >= extra) p[u * step + i] = v[u].v[i];
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < N; u++) {
+        if constexpr (PAST && sizeof(v[0]) == 16) {
+            raw16 w;
+            __builtin_memcpy(&w, &v[u], 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<raw16 *>(p + u * step));
+        } else {
+            store_vec<T, V>(p + u * step, v[u]);
+        }
     }
 }
 
@@ -184,32 +195,33 @@ static_assert(kNormBlocks <= kJoinWays * kJoinWays && kNormCounters >= 1 + kJoin
 __device__ __forceinline__ int group_of(int c, float inv_cpg) { return (int)(((float)c + 0.5f) * inv_cpg); }
 
 // A vector's channels: their groups' statistics (one group's where V divides
-// the channels of a group: GROUPED), and gamma and beta.
+// the channels of a group: GROUPED), and gamma and beta.  (OVER, below: V does
+// not divide a row, see Columns.)
 template <int V, bool GROUPED>
 struct Channels {
     float mean_[GROUPED ? 1 : V], rstd_[GROUPED ? 1 : V], scale[V], beta[V];     // scale = rstd gamma
     __device__ __forceinline__ float mean(int v) const { return mean_[GROUPED ? 0 : v]; }
     __device__ __forceinline__ float rstd(int v) const { return rstd_[GROUPED ? 0 : v]; }
-    __device__ __forceinline__ Channels(const NormArgs &a, int b, int col)
+    __device__ __forceinline__ Channels(const NormArgs &a, int b, int first)
     {
         const float inv_cpg = 1.0f / (float)(a.channels / a.groups);
         const float2 *stats = reinterpret_cast<const float2 *>(a.stats) + (int64_t)b * a.groups;
 #pragma unroll
         for (int v = 0; v < (GROUPED ? 1 : V); v++) {
-            const float2 st = stats[group_of(col * V + v, inv_cpg)];
+            const float2 st = stats[group_of(first + v, inv_cpg)];
             mean_[v] = st.x;
             rstd_[v] = st.y;
         }
-        load(a, col);
+        load(a, first);
     }
-    __device__ __forceinline__ Channels(const NormArgs &a, float mean, float rstd, int col)
+    __device__ __forceinline__ Channels(const NormArgs &a, float mean, float rstd, int first)
     {
         static_assert(GROUPED, "one group's statistics");
         mean_[0] = mean;
         rstd_[0] = rstd;
-        load(a, col);
+        load(a, first);
     }
-    __device__ __forceinline__ void load(const NormArgs &a, int col)
+    __device__ __forceinline__ void load(const NormArgs &a, int first)
     {
         Vec<float, V> g, s;
 #pragma unroll
@@ -217,8 +229,8 @@ struct Channels {
             g.v[v] = 1.0f;
             s.v[v] = 0.0f;
         }
-        if (a.gamma) g = load_vec<float, V>(a.gamma + col * V);
-        if (a.beta) s = load_vec<float, V>(a.beta + col * V);
+        if (a.gamma) g = load_vec<float, V>(a.gamma + first);
+        if (a.beta) s = load_vec<float, V>(a.beta + first);
 #pragma unroll
         for (int v = 0; v < V; v++) {
             scale[v] = rstd(v) * g.v[v];
@@ -230,10 +242,10 @@ struct Channels {
 // How a workgroup covers a row of C channels.
 template <int V>
 struct Columns {
-    int per_row, rows, col, row;     // vectors in a row, rows at a time, this thread's first vector and row
-    __device__ __forceinline__ explicit Columns(int channels)
+    int channels, per_row, rows, col, row;     // vectors in a row, rows at a time, this thread's first vector and row
+    __device__ __forceinline__ explicit Columns(int channels_) : channels(channels_)
     {
-        per_row = channels / V;
+        per_row = (channels + V - 1) / V;
         rows = per_row >= kNormThreads ? 1 : kNormThreads / per_row;
         if (rows == 1) {
             row = 0;
@@ -244,6 +256,14 @@ struct Columns {
             if (row >= rows) col = per_row;        // left over: no column
         }
     }
+    // The first channel of vector `col`.  Where V does not divide a row its last
+    // vector is the row's last V channels; the first extra(col) of them are the
+    // vector before's as well, which alone counts and writes them.
+    __device__ __forceinline__ int first(int col) const
+    {
+        return col * V + V <= channels ? col * V : channels - V;
+    }
+    __device__ __forceinline__ int extra(int col) const { return col * V - first(col); }
 };
 
 // Lanes that share one group's sum: a power of two, at most a wave.
@@ -281,7 +301,7 @@ __device__ __forceinline__ void for_chunks(const Columns<V> &cols, int rows, int
 }
 
 // Partial statistics: part[b][block][g] = (mean, M2) over the block's rows.
-template <typename T, int V, bool GROUPED>
+template <typename T, int V, bool GROUPED, bool OVER>
 __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
 {
     // units of U channels of one group: a thread's vector, or a channel
@@ -294,7 +314,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
     float *lmean = lds, *lm2 = lds + cols.rows * units;
     const T *x = static_cast<const T *>(a.x) + b * a.x_sample;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const T *p = x + col * V;
+        const int first = OVER ? cols.first(col) : col * V, extra = OVER ? cols.extra(col) : 0;
+        const T *p = x + first;
         const int64_t step = cols.rows * a.x_ld;
         int n = 0;
         float shift[V], s1[V], s2[V];
@@ -335,7 +356,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
             mean[v] = fmaf(s1[v], inv, shift[v]);
             m2[v] = s2[v] - s1[v] * s1[v] * inv;
         }
-        const int at = cols.row * units + col * (V / U);
+        const int at = cols.row * units + first / U;
         if constexpr (GROUPED) {
             float m = 0.0f, q = 0.0f;
 #pragma unroll
@@ -347,10 +368,11 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
             lm2[at] = q;
         } else {
 #pragma unroll
-            for (int v = 0; v < V; v++) {
-                lmean[at + v] = mean[v];
-                lm2[at + v] = m2[v];
-            }
+            for (int v = 0; v < V; v++)
+                if (v >= extra) {
+                    lmean[at + v] = mean[v];
+                    lm2[at + v] = m2[v];
+                }
         }
         if (col == 0) counts[cols.row] = (float)(n * U);
     }
@@ -404,16 +426,17 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
 
 // y = act((x - mean) (rstd gamma) + beta); pixels from the sample's count on
 // are set to 0.
-template <typename T, int V, bool GROUPED, bool PAST, int ACT>
+template <typename T, int V, bool GROUPED, bool OVER, bool PAST, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 {
     const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
     const Columns<V> cols(a.channels);
     const int pb = valid_pixels(a, b);
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + col * V;
-        T *y = static_cast<T *>(a.out) + b * a.out_sample + col * V;
-        const Channels<V, GROUPED> ch(a, b, col);
+        const int first = OVER ? cols.first(col) : col * V, extra = OVER ? cols.extra(col) : 0;
+        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + first;
+        T *y = static_cast<T *>(a.out) + b * a.out_sample + first;
+        const Channels<V, GROUPED> ch(a, b, first);
         auto one = [&](const Vec<T, V> &f) {
             Vec<T, V> o;
 #pragma unroll
@@ -430,14 +453,15 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 #pragma unroll
                 for (int u = 0; u < kNormUnroll; u++) f[u] = load_vec<T, V>(px + u * xs);
 #pragma unroll
-                for (int u = 0; u < kNormUnroll; u++) store_map<PAST>(py + u * ys, one(f[u]));
+                for (int u = 0; u < kNormUnroll; u++) f[u] = one(f[u]);
+                store_map<PAST>(py, ys, f, extra);
             } else {
                 for (int u = 0; u < count; u++) {
-                    Vec<T, V> o;
+                    Vec<T, V> o[1];
 #pragma unroll
-                    for (int v = 0; v < V; v++) o.v[v] = (T)0.0f;
-                    if (r + u * cols.rows < pb) o = one(load_vec<T, V>(px + u * xs));
-                    store_map<PAST>(py + u * ys, o);
+                    for (int v = 0; v < V; v++) o[0].v[v] = (T)0.0f;
+                    if (r + u * cols.rows < pb) o[0] = one(load_vec<T, V>(px + u * xs));
+                    store_map<PAST>(py + u * ys, 0, o, extra);
                 }
             }
         });
@@ -445,7 +469,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 }
 
 // part[b][block][c] = (sum du, sum du xh) over the block's rows.
-template <typename T, int V, bool GROUPED, int ACT>
+template <typename T, int V, bool GROUPED, bool OVER, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
 {
     extern __shared__ float lds[];      // [rows][C] sums of du, then of du xh
@@ -454,9 +478,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
     const Columns<V> cols(C);
     float *l1 = lds, *l2 = lds + cols.rows * C;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const Channels<V, GROUPED> ch(a, b, col);
-        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + col * V;
-        const T *dy = static_cast<const T *>(a.dy) + b * a.dy_sample + col * V;
+        const int first = OVER ? cols.first(col) : col * V, extra = OVER ? cols.extra(col) : 0;
+        const Channels<V, GROUPED> ch(a, b, first);
+        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + first;
+        const T *dy = static_cast<const T *>(a.dy) + b * a.dy_sample + first;
         const int64_t xs = cols.rows * a.x_ld, ds = cols.rows * a.dy_ld;
         float s1[V], s2[V];
 #pragma unroll
@@ -486,11 +511,12 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
             }
         });
 #pragma unroll
-        for (int v = 0; v < V; v++) {
-            const int at = cols.row * C + col * V + v;
-            l1[at] = s1[v];
-            l2[at] = s2[v] * ch.rstd(v);
-        }
+        for (int v = 0; v < V; v++)
+            if (v >= extra) {
+                const int at = cols.row * C + first + v;
+                l1[at] = s1[v];
+                l2[at] = s2[v] * ch.rstd(v);
+            }
     }
     __syncthreads();
     for (int c = threadIdx.x; c < C; c += kNormThreads) {
@@ -581,7 +607,7 @@ __device__ __forceinline__ float grad_one(const Channels<V, GROUPED> &ch, int v,
 }
 
 // dx, and (the first `vectors` workgroups) dgamma and dbeta.
-template <typename T, int V, bool GROUPED, bool PAST, int ACT>
+template <typename T, int V, bool GROUPED, bool OVER, bool PAST, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a, int vectors)
 {
     if ((int)blockIdx.x < vectors) {
@@ -594,12 +620,13 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a, in
     const float inv_cpg = 1.0f / (float)(a.channels / a.groups);
     const float2 *sums = reinterpret_cast<const float2 *>(a.group_sums) + (int64_t)b * a.groups;
     for (int col = cols.col; col < cols.per_row; col += kNormThreads) {
-        const Channels<V, GROUPED> ch(a, b, col);
+        const int first = OVER ? cols.first(col) : col * V, extra = OVER ? cols.extra(col) : 0;
+        const Channels<V, GROUPED> ch(a, b, first);
         constexpr int N = GROUPED ? 1 : V;
         float flat[N], slope[N];
 #pragma unroll
         for (int v = 0; v < N; v++) {
-            const float2 aq = sums[group_of(col * V + v, inv_cpg)];       // a / n and q / n
+            const float2 aq = sums[group_of(first + v, inv_cpg)];       // a / n and q / n
             flat[v] = -ch.rstd(v) * aq.x;
             slope[v] = -ch.rstd(v) * ch.rstd(v) * aq.y;
         }
@@ -611,9 +638,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a, in
                                           slope[GROUPED ? 0 : v]);
             return o;
         };
-        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + col * V;
-        const T *dy = static_cast<const T *>(a.dy) + b * a.dy_sample + col * V;
-        T *dx = static_cast<T *>(a.out) + b * a.out_sample + col * V;
+        const T *x = static_cast<const T *>(a.x) + b * a.x_sample + first;
+        const T *dy = static_cast<const T *>(a.dy) + b * a.dy_sample + first;
+        T *dx = static_cast<T *>(a.out) + b * a.out_sample + first;
         const int64_t xs = cols.rows * a.x_ld, ds = cols.rows * a.dy_ld, os = cols.rows * a.out_ld;
         for_chunks<true, V>(cols, a.pixels, a.blocks, i, [&](int64_t r, int count) {
             const T *px = x + r * a.x_ld, *pd = dy + r * a.dy_ld;
@@ -626,14 +653,15 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a, in
                     fd[u] = load_vec<T, V>(pd + u * ds);
                 }
 #pragma unroll
-                for (int u = 0; u < kNormUnroll; u++) store_map<PAST>(po + u * os, one(fx[u], fd[u]));
+                for (int u = 0; u < kNormUnroll; u++) fx[u] = one(fx[u], fd[u]);
+                store_map<PAST>(po, os, fx, extra);
             } else {
                 for (int u = 0; u < count; u++) {
-                    Vec<T, V> o;
+                    Vec<T, V> o[1];
 #pragma unroll
-                    for (int v = 0; v < V; v++) o.v[v] = (T)0.0f;
-                    if (r + u * cols.rows < pb) o = one(load_vec<T, V>(px + u * xs), load_vec<T, V>(pd + u * ds));
-                    store_map<PAST>(po + u * os, o);
+                    for (int v = 0; v < V; v++) o[0].v[v] = (T)0.0f;
+                    if (r + u * cols.rows < pb) o[0] = one(load_vec<T, V>(px + u * xs), load_vec<T, V>(pd + u * ds));
+                    store_map<PAST>(po + u * os, 0, o, extra);
                 }
             }
         });
@@ -738,7 +766,7 @@ __global__ __launch_bounds__(kGroupThreads) void k_norm_group(NormArgs a)
     const float var = m2 > 0.0f || m2 != m2 ? m2 / n : 0.0f;
     const float rstd = (float)(1.0 / sqrt((double)var + (double)a.eps));
     if (threadIdx.x == 0) reinterpret_cast<float2 *>(a.stats)[at.b * a.groups + at.g] = make_float2(mean, rstd);
-    const Channels<V, true> ch(a, mean, rstd, at.row < at.rows ? col : 0);
+    const Channels<V, true> ch(a, mean, rstd, at.row < at.rows ? col * V : 0);
     as_loaded(held);
 #pragma unroll
     for (int k = 0; k < K; k++) {
@@ -774,7 +802,7 @@ __global__ __launch_bounds__(kGroupThreads) void k_norm_grad_group(NormArgs a)
     as_loaded(hx);
     as_loaded(hd);
     const float2 st = reinterpret_cast<const float2 *>(a.stats)[at.b * a.groups + at.g];
-    const Channels<V, true> ch(a, st.x, st.y, at.row < at.rows ? col : 0);
+    const Channels<V, true> ch(a, st.x, st.y, at.row < at.rows ? col * V : 0);
     float sum[2][V];
 #pragma unroll
     for (int v = 0; v < V; v++) sum[0][v] = sum[1][v] = 0.0f;
@@ -868,37 +896,38 @@ bool aligned_rows(const NormArgs &a)
     return aligned_to(a.out, 16) && a.out_ld % E == 0 && (a.samples == 1 || a.out_sample % E == 0);
 }
 
-template <typename T, int V, bool GROUPED, int ACT>
+template <typename T, int V, bool GROUPED, bool OVER, int ACT>
 hipError_t launch_norm(NormArgs a, hipStream_t stream)
 {
-    const int rows = a.channels / V >= kNormThreads ? 1 : kNormThreads / (a.channels / V);
+    const int per_row = (int)ceil_div(a.channels, V), rows = per_row >= kNormThreads ? 1 : kNormThreads / per_row;
     const size_t least = 2 * sizeof(double) * kNormThreads;       // (the join's)
     const size_t whole = 2 * sizeof(float) * (size_t)rows * a.channels, units = GROUPED ? whole / V : whole;
     const size_t lds = a.backward ? whole : units;
     a.chunk = rows * kNormUnroll;
     a.blocks = a.samples > 0 ? blocks_per_sample(a) : 0;
     const int64_t bytes = (int64_t)a.samples * a.pixels * a.channels * (int64_t)sizeof(T);
-    const bool past = V * sizeof(T) == 16 && bytes * (a.backward ? 3 : 2) > kCacheBytes && aligned_rows<T>(a);
+    constexpr bool kCanPast = V * sizeof(T) == 16 && !OVER;
+    const bool past = kCanPast && bytes * (a.backward ? 3 : 2) > kCacheBytes && aligned_rows<T>(a);
     const dim3 grid(a.samples * a.blocks), block(kNormThreads);
     if (!a.backward) {
-        hipLaunchKernelGGL((k_norm_stats<T, V, GROUPED>), grid, block, lds > least ? lds : least, stream, a);
+        hipLaunchKernelGGL((k_norm_stats<T, V, GROUPED, OVER>), grid, block, lds > least ? lds : least, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         if (past)
-            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, V * sizeof(T) == 16, ACT>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, OVER, kCanPast, ACT>), grid, block, 0, stream, a);
         else
-            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, false, ACT>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((k_norm_apply<T, V, GROUPED, OVER, false, ACT>), grid, block, 0, stream, a);
         return hipGetLastError();
     }
     const int vectors = a.dgamma || a.dbeta ? (int)ceil_div(a.channels, kVectorChannels) : 0;
     if (a.samples > 0) {
-        hipLaunchKernelGGL((k_norm_grad_sums<T, V, GROUPED, ACT>), grid, block, lds > least ? lds : least, stream, a);
+        hipLaunchKernelGGL((k_norm_grad_sums<T, V, GROUPED, OVER, ACT>), grid, block, lds > least ? lds : least, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (a.samples > 0 && a.out && past)
-        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, V * sizeof(T) == 16, ACT>), dim3(grid.x + vectors), block,
+        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, OVER, kCanPast, ACT>), dim3(grid.x + vectors), block,
                            0, stream, a, vectors);
     else if (a.samples > 0 && a.out)
-        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, false, ACT>), dim3(grid.x + vectors), block, 0, stream, a,
+        hipLaunchKernelGGL((k_norm_grad_apply<T, V, GROUPED, OVER, false, ACT>), dim3(grid.x + vectors), block, 0, stream, a,
                            vectors);
     else
         hipLaunchKernelGGL(k_norm_grad_vectors<0>, dim3(vectors), block, 0, stream, a);
@@ -962,15 +991,13 @@ hipError_t launch_norm_act(const NormArgs &a, hipStream_t stream)
         if (group_fits<T, 8>(a)) return launch_group<T, 8, ACT>(a, stream);
     if (group_fits<T, 4>(a)) return launch_group<T, 4, ACT>(a, stream);
     if (group_fits<T, 1>(a)) return launch_group<T, 1, ACT>(a, stream);
-    // two passes, in the widest vectors that divide a row
-    if constexpr (sizeof(T) == 2) {
-        if (cpg % 8 == 0) return launch_norm<T, 8, true, ACT>(a, stream);
-        if (C % 8 == 0) return launch_norm<T, 8, false, ACT>(a, stream);
-    }
-    if (cpg % 4 == 0) return launch_norm<T, 4, true, ACT>(a, stream);
-    if (C % 4 == 0) return launch_norm<T, 4, false, ACT>(a, stream);
-    if (C % 2 == 0) return launch_norm<T, 2, false, ACT>(a, stream);
-    return launch_norm<T, 1, true, ACT>(a, stream);
+    // two passes, in 16-byte vectors (1000 x 1000 pixels of 25 channels in bf16: 30 us
+    // in vectors of one)
+    constexpr int E = 16 / (int)sizeof(T);
+    if (cpg % E == 0) return launch_norm<T, E, true, false, ACT>(a, stream);
+    if (C % E == 0) return launch_norm<T, E, false, false, ACT>(a, stream);
+    if (C >= E) return launch_norm<T, E, false, true, ACT>(a, stream);
+    return launch_norm<T, 1, true, false, ACT>(a, stream);
 }
 
 template <typename T>
