@@ -594,13 +594,13 @@ __global__ __launch_bounds__(256, 2) void k_gemm_narrow(GemmArgs g)
 }
 
 // dz = dy act'(preact), rounded (the products' operand), and its column sums
-// over this workgroup's rows, unrounded.  A workgroup covers up to 256 vectors
+// over this workgroup's rows, unrounded.  A workgroup covers g.slab vectors
 // of V columns (blockIdx.y) and 256 / vectors rows at a time.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
 {
     __shared__ float lds[256 * V];
-    const int all = g.n / V, first = blockIdx.y * 256, here = all - first < 256 ? all - first : 256;
+    const int all = g.n / V, first = blockIdx.y * g.slab, here = all - first < g.slab ? all - first : g.slab;
     const int rows = 256 / here, row = threadIdx.x / here, col = threadIdx.x - row * here;
     const int64_t span = (g.rows + (int64_t)g.blocks - 1) / g.blocks, lo = span * blockIdx.x;
     const int64_t hi = lo + span < g.rows ? lo + span : g.rows;
@@ -642,10 +642,11 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
     }
     __syncthreads();
     if (!g.sums) return;
+    float *out = g.blocks == 1 ? g.sums : g.part + (int64_t)blockIdx.x * g.n;
     for (int i = threadIdx.x; i < here * V; i += 256) {
         float s = 0.0f;
         for (int r = 0; r < rows; r++) s += lds[r * here * V + i];
-        g.part[(int64_t)blockIdx.x * g.n + first * V + i] = s;
+        out[first * V + i] = s;
     }
 }
 
@@ -692,7 +693,7 @@ __device__ __forceinline__ int strip_swizzle(int row, int chunks)
 }
 
 template <typename T, int NT, int KT, int ACT>
-__global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(NarrowGradArgs a)
+__global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs a)
 {
     constexpr int kZChunks = NT * 2, kXChunks = KT * 16;                  // chunks of an LDS row
     constexpr int kZBytes = kStripRows * kZChunks * 16, kXBytes = kStripRows * kXChunks * 16;
@@ -866,6 +867,126 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(NarrowGradArg
     }
 }
 
+// The gradient of few rows (at most 64): dz is formed where it is needed, since
+// there is little of it, and neither scratch nor a join is.
+//
+// dx: 16 columns per workgroup, its waves dividing n; w's column of each lane is
+// gathered, sixteen lanes side by side.
+template <typename T, int MT, int ACT>
+__global__ __launch_bounds__(1024) void k_rows_dx(WholeGradArgs a)
+{
+    __shared__ f32x4 joined[16][MT][64];
+    constexpr int E = kChunk<T>, kStep = 4 * E;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const int j = lane & 15, c = lane >> 4, k = blockIdx.x * 16 + j;
+    const int steps = (a.n + kStep - 1) / kStep, each = (steps + waves - 1) / waves;
+    const int lo = wave * each, hi = lo + each < steps ? lo + each : steps;
+    const T *w = static_cast<const T *>(a.w) + (k < a.k ? k : a.k - 1);      // (columns that are not there: the last)
+    f32x4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; i++) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = lo; s < hi; s++) {
+        const int n0 = s * kStep + c * E, left = a.n - n0;
+        Fragment fw, fz[MT];
+        T e[E];
+#pragma unroll
+        for (int i = 0; i < E; i++) e[i] = i < left ? w[(n0 + i) * a.ldw] : (T)0.0f;
+        __builtin_memcpy(&fw, e, 16);
+#pragma unroll
+        for (int t = 0; t < MT; t++) {
+            const int m = 16 * t + j, here = m < a.rows ? left : 0;
+            fz[t].u = load_chunk<T>(static_cast<const T *>(a.dy) + m * a.ldd + n0, here);
+            if constexpr (ACT != CPE_ACT_NONE) {
+                Fragment z;
+                z.u = load_chunk<T>(static_cast<const T *>(a.preact) + m * a.ldp + n0, here);
+                T ez[E];
+                __builtin_memcpy(e, &fz[t], 16);
+                __builtin_memcpy(ez, &z, 16);
+#pragma unroll
+                for (int i = 0; i < E; i++) e[i] = (T)((float)e[i] * activate_grad<ACT>((float)ez[i]));
+                __builtin_memcpy(&fz[t], e, 16);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < MT; t++) acc[t] = mma<T>(fw, fz[t], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; t++) joined[wave][t][lane] = acc[t];
+    __syncthreads();
+    if (wave < MT) {
+        f32x4 v = joined[0][wave][lane];
+        for (int i = 1; i < waves; i++) v += joined[i][wave][lane];
+        const int m = 16 * wave + j, k4 = blockIdx.x * 16 + 4 * c;
+        if (m < a.rows) {
+            T *out = static_cast<T *>(a.dx) + m * a.lddx + k4;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (k4 + i < a.k) out[i] = (T)v[i];
+        }
+    }
+}
+
+// dw and dbias: 64 n by 64 k per workgroup, 16 n of them per wave.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void k_rows_dw(WholeGradArgs a)
+{
+    constexpr int E = kChunk<T>, kStep = 4 * E;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const int n = blockIdx.y * 64 + wave * 16 + j, k0 = blockIdx.x * 64;
+    const bool n_on = n < a.n;
+    f32x4 acc[4];
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; t++) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int m0 = c * E; m0 < (a.rows + kStep - 1) / kStep * kStep; m0 += kStep) {
+        Fragment fz, fx[4];
+        T e[E];
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            const int m = m0 + i;
+            float dz = 0.0f;
+            if (n_on && m < a.rows) {
+                dz = (float)static_cast<const T *>(a.dy)[m * a.ldd + n];
+                if constexpr (ACT != CPE_ACT_NONE)
+                    dz *= activate_grad<ACT>((float)static_cast<const T *>(a.preact)[m * a.ldp + n]);
+            }
+            sum += dz;
+            e[i] = (T)dz;
+        }
+        __builtin_memcpy(&fz, e, 16);
+        if (!a.dw) continue;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const int k = k0 + 16 * t + j;
+#pragma unroll
+            for (int i = 0; i < E; i++)
+                e[i] = k < a.k && m0 + i < a.rows ? static_cast<const T *>(a.x)[(m0 + i) * a.ldx + k] : (T)0.0f;
+            __builtin_memcpy(&fx[t], e, 16);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; t++) acc[t] = mma<T>(fx[t], fz, acc[t]);
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (a.dbias && blockIdx.x == 0 && c == 0 && n_on) a.dbias[n] = sum;
+    if (!a.dw || !n_on) return;
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        const int k = k0 + 16 * t + 4 * c;
+        T *out = static_cast<T *>(a.dw) + n * a.lddw + k;
+        if (k + 4 <= a.k) {
+            Vec<T, 4> o;
+#pragma unroll
+            for (int i = 0; i < 4; i++) o.v[i] = (T)acc[t][i];
+            store_vec<T, 4>(out, o);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (k + i < a.k) out[i] = (T)acc[t][i];
+        }
+    }
+}
+
 // -- launches -----------------------------------------------------------------------
 
 template <typename T>
@@ -1020,10 +1141,19 @@ hipError_t launch_gemm_type(const GemmArgs &all, hipStream_t stream)
 template <typename T, int V>
 hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
 {
-    const int vectors = g.n / V, rows = vectors >= 256 ? 1 : 256 / vectors;
-    const int64_t slabs = ceil_div(vectors, 256);
-    const int64_t want = ceil_div(g.rows, 4 * (int64_t)rows), cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
-    g.blocks = (int32_t)(want < 1 ? 1 : want < cap ? want : cap);
+    // few enough rows for one workgroup per slab of 32 vectors: no join
+    const int vectors = g.n / V;
+    g.slab = 32;
+    int rows = 256 / (vectors < g.slab ? vectors : g.slab);
+    g.blocks = 1;
+    if (g.rows > 16 * rows) {
+        g.slab = 256;
+        rows = vectors >= 256 ? 1 : 256 / vectors;
+        const int64_t slabs = ceil_div(vectors, 256);
+        const int64_t want = ceil_div(g.rows, 4 * (int64_t)rows), cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
+        g.blocks = (int32_t)(want < 1 ? 1 : want < cap ? want : cap);
+    }
+    const int64_t slabs = ceil_div(vectors, g.slab);
     const dim3 grid(g.blocks, (unsigned)slabs);
     switch (g.act) {
     case CPE_ACT_RELU: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_RELU>), grid, dim3(256), 0, stream, g); break;
@@ -1031,7 +1161,7 @@ hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
     case CPE_ACT_GELU: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_GELU>), grid, dim3(256), 0, stream, g); break;
     default: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_NONE>), grid, dim3(256), 0, stream, g); break;
     }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !g.sums) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !g.sums || g.blocks == 1) return e;
     hipLaunchKernelGGL(k_column_join, dim3((unsigned)ceil_div(g.n, 32)), dim3(1024), 0, stream, g);
     return hipGetLastError();
 }
@@ -1048,7 +1178,7 @@ hipError_t launch_grad_type(const GradArgs &g, hipStream_t stream)
 
 // dw and dbias over the workgroups' partials, four values per 16 lanes.
 template <typename T>
-__global__ __launch_bounds__(256) void k_narrow_grad_join(NarrowGradArgs a)
+__global__ __launch_bounds__(256) void k_narrow_grad_join(WholeGradArgs a)
 {
     __shared__ f32x4 lds[16][16];
     const int at = threadIdx.x & 15, lane = threadIdx.x >> 4;
@@ -1079,7 +1209,7 @@ __global__ __launch_bounds__(256) void k_narrow_grad_join(NarrowGradArgs a)
 }
 
 template <typename T, int NT, int KT>
-hipError_t launch_narrow_grad_size(const NarrowGradArgs &a, hipStream_t stream)
+hipError_t launch_narrow_grad_size(const WholeGradArgs &a, hipStream_t stream)
 {
     const dim3 grid(a.blocks), block(kNarrowThreads);
     switch (a.act) {
@@ -1092,7 +1222,7 @@ hipError_t launch_narrow_grad_size(const NarrowGradArgs &a, hipStream_t stream)
 }
 
 template <typename T>
-hipError_t launch_narrow_grad_type(NarrowGradArgs a, hipStream_t stream)
+hipError_t launch_narrow_grad_type(WholeGradArgs a, hipStream_t stream)
 {
     // one workgroup per CU: a second one would double the partial dw
     const int64_t strips = ceil_div(a.rows, kStripRows);
@@ -1109,6 +1239,38 @@ hipError_t launch_narrow_grad_type(NarrowGradArgs a, hipStream_t stream)
     const int64_t quads = (a.dw ? (int64_t)a.n * (a.k / 4) : 0) + (a.dbias ? a.n / 4 : 0);
     hipLaunchKernelGGL(k_narrow_grad_join<T>, dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename T, int ACT>
+hipError_t launch_rows_grad(const WholeGradArgs &a, hipStream_t stream)
+{
+    if (a.dx) {
+        const int steps = (int)ceil_div(a.n, 4 * kChunk<T>);
+        const int waves = steps >= 64 ? 16 : steps >= 16 ? 8 : 4;
+        const dim3 grid((unsigned)ceil_div(a.k, 16)), block(64 * waves);
+        if (a.rows <= 16)
+            hipLaunchKernelGGL((k_rows_dx<T, 1, ACT>), grid, block, 0, stream, a);
+        else if (a.rows <= 32)
+            hipLaunchKernelGGL((k_rows_dx<T, 2, ACT>), grid, block, 0, stream, a);
+        else
+            hipLaunchKernelGGL((k_rows_dx<T, 4, ACT>), grid, block, 0, stream, a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (!a.dw && !a.dbias) return hipSuccess;
+    const dim3 grid(a.dw ? (unsigned)ceil_div(a.k, 64) : 1u, (unsigned)ceil_div(a.n, 64));
+    hipLaunchKernelGGL((k_rows_dw<T, ACT>), grid, dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_rows_grad_type(const WholeGradArgs &a, hipStream_t stream)
+{
+    switch (a.act) {
+    case CPE_ACT_RELU: return launch_rows_grad<T, CPE_ACT_RELU>(a, stream);
+    case CPE_ACT_SILU: return launch_rows_grad<T, CPE_ACT_SILU>(a, stream);
+    case CPE_ACT_GELU: return launch_rows_grad<T, CPE_ACT_GELU>(a, stream);
+    default: return launch_rows_grad<T, CPE_ACT_NONE>(a, stream);
+    }
 }
 
 }  // namespace

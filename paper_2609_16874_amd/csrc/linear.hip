@@ -54,10 +54,21 @@ constexpr int kNarrowGradRows = 4096;
 }  // namespace
 
 namespace cpe {
-bool narrow_grad_fits(const NarrowGradArgs &a)
+bool narrow_grad_fits(const WholeGradArgs &a)
 {
     if (a.rows < kNarrowGradRows || a.n % 8 != 0 || a.k % 8 != 0) return false;
     return (a.n <= 128 && a.k <= 256) || (a.n <= 64 && a.k <= 512);
+}
+// Few rows: two launches instead of four or five, 14 us against 20 on small
+// products (calls as a program makes them).  Every workgroup forms the dz that
+// it needs again and gathers w's columns, which costs more than that on larger
+// ones: bf16 16 x 2048 to 4096 46 us against 33, 64 x 1024 to 1024 29 against
+// 27; binary32, whose tiles waste more on rows that are not there, 23 x 3776 to
+// 1152 28 against 39.
+bool rows_grad_fits(const WholeGradArgs &a, cpe_dtype dtype)
+{
+    const int64_t most = (int64_t)1 << (dtype == CPE_F32 ? 27 : 25);
+    return a.rows >= 1 && a.rows <= 64 && (int64_t)a.rows * a.n * a.k <= most;
 }
 }  // namespace cpe
 
@@ -155,8 +166,8 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
     }
     if (dw && !check_matrix(h, dw, dw_ld, h->in)) return CPE_ERR_INVALID_ARG;
     (void)hipGetLastError();
-    if (h->dtype != CPE_F32) {
-        NarrowGradArgs a{};
+    {
+        WholeGradArgs a{};
         a.x = x;
         a.ldx = x_ld;
         a.w = w;
@@ -176,7 +187,13 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
         a.n = h->out;
         a.k = h->in;
         a.act = h->act;
-        if (narrow_grad_fits(a)) {
+        if (rows_grad_fits(a, h->dtype)) {
+            const hipError_t e = h->dtype == CPE_F32   ? launch_rows_grad_f32(a, stream)
+                                 : h->dtype == CPE_F16 ? launch_rows_grad_f16(a, stream)
+                                                       : launch_rows_grad_bf16(a, stream);
+            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
+        }
+        if (h->dtype != CPE_F32 && narrow_grad_fits(a)) {
             const hipError_t e = h->dtype == CPE_F16 ? launch_narrow_grad_f16(a, stream)
                                                      : launch_narrow_grad_bf16(a, stream);
             return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;

@@ -41,13 +41,13 @@ struct GradArgs {
     int64_t ldd, ldp, ldz;
     void *dz;
     float *part, *sums;                       // scratch [blocks][n]; out [n]
-    int32_t rows, n, blocks;
+    int32_t rows, n, blocks, slab;            // workgroups along the rows, vectors of columns of each
     int act;
 };
 
-// A narrow product's whole gradient: dz = dy act'(preact), dx = dz w,
+// A narrow or few-row product's whole gradient: dz = dy act'(preact), dx = dz w,
 // dw = dz^T x, dbias = column sums of dz; those whose pointer is not null.
-struct NarrowGradArgs {
+struct WholeGradArgs {
     const void *x, *w, *dy, *preact;
     int64_t ldx, ldw, ldd, ldp, lddx, lddw;
     void *dx, *dw;
@@ -64,8 +64,13 @@ hipError_t launch_grad_f32(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_f16(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_bf16(const GradArgs &g, hipStream_t stream);
 // whether the gradient is done in one pass (16-bit types), and that pass
-bool narrow_grad_fits(const NarrowGradArgs &a);
-hipError_t launch_narrow_grad_f16(NarrowGradArgs a, hipStream_t stream);
-hipError_t launch_narrow_grad_bf16(NarrowGradArgs a, hipStream_t stream);
+bool narrow_grad_fits(const WholeGradArgs &a);
+hipError_t launch_narrow_grad_f16(WholeGradArgs a, hipStream_t stream);
+hipError_t launch_narrow_grad_bf16(WholeGradArgs a, hipStream_t stream);
+// whether there are few rows, and the gradient of those
+bool rows_grad_fits(const WholeGradArgs &a, cpe_dtype dtype);
+hipError_t launch_rows_grad_f32(const WholeGradArgs &a, hipStream_t stream);
+hipError_t launch_rows_grad_f16(const WholeGradArgs &a, hipStream_t stream);
+hipError_t launch_rows_grad_bf16(const WholeGradArgs &a, hipStream_t stream);
 
 }  // namespace cpe

@@ -20,6 +20,7 @@ SHAPES = [
     (64, 72, 40, 0), (65, 64, 128, 0), (128, 128, 128, 0), (129, 100, 65, 3), (200, 8, 4, 0), (300, 257, 131, 0),
     (257, 520, 136, 24), (1000, 64, 200, 0), (100, 4096, 96, 0), (90, 2049, 130, 0), (5000, 24, 8, 0),
     (12345, 48, 40, 0), (4100, 256, 128, 0), (4097, 512, 64, 8), (6001, 200, 120, 0), (9000, 136, 16, 5), (5000, 304, 40, 0),
+    (2, 520, 1032, 0), (33, 130, 70, 5), (64, 1000, 264, 0), (48, 96, 2500, 0),
 ]
 
 
