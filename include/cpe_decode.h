@@ -86,8 +86,7 @@ typedef enum {
     CPE_ERR_HIP = 4
 } cpe_status;
 
-/* CPE_BF16 is a type of the operators of cpe_head.h; the decoder reads the other two. */
-typedef enum { CPE_F32 = 0, CPE_F16 = 1, CPE_BF16 = 2 } cpe_dtype;
+typedef enum { CPE_F32 = 0, CPE_F16 = 1 } cpe_dtype;
 
 /* One decoded centroid (32 bytes). */
 typedef struct {

@@ -5,8 +5,8 @@
  * activation and residual that projects a map's features to its embedding
  * (or a block's features to the next one's), each with its gradient.
  *
- * Types.  Maps and weight matrices have the handle's dtype (CPE_F32, CPE_F16
- * or CPE_BF16); per-channel vectors (gamma, beta, bias, their gradients) and
+ * Types.  Maps and weight matrices have the handle's dtype (f32, f16 or bf16; the
+ * decoder reads the first two); per-channel vectors (gamma, beta, bias, their gradients) and
  * group statistics are float.  Sums, statistics and activations are formed in
  * binary32 and each output is rounded once, to nearest even; where a product's
  * operand is an intermediate result, its entry says how it is held.
@@ -44,6 +44,9 @@
 extern "C" {
 #endif
 
+/* (f32 and f16 have the codes of cpe_dtype) */
+typedef enum { CPE_HEAD_F32 = 0, CPE_HEAD_F16 = 1, CPE_HEAD_BF16 = 2 } cpe_head_dtype;
+
 typedef enum { CPE_ACT_NONE = 0, CPE_ACT_RELU = 1, CPE_ACT_SILU = 2, CPE_ACT_GELU = 3 } cpe_activation;
 
 typedef struct cpe_norm cpe_norm;
@@ -64,7 +67,7 @@ typedef struct cpe_linear cpe_linear;
  *   eps           finite, > 0
  */
 cpe_status cpe_norm_create(cpe_norm **out, int32_t max_samples, int32_t max_pixels, int32_t channels,
-                           int32_t groups, cpe_dtype dtype, cpe_activation act, float eps);
+                           int32_t groups, cpe_head_dtype dtype, cpe_activation act, float eps);
 
 /*
  * y = act(norm(x)), asynchronously on `stream`.
@@ -106,7 +109,7 @@ size_t cpe_norm_workspace_bytes(const cpe_norm *h);
  *   in_features    K, 1..65536; out_features N, 1..65536
  */
 cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_features, int32_t out_features,
-                             cpe_dtype dtype, cpe_activation act);
+                             cpe_head_dtype dtype, cpe_activation act);
 
 /*
  * y [rows][N] from x [rows][K] and w [N][K], asynchronously on `stream`.

@@ -1,8 +1,9 @@
 """Compile the gfx950 HIP library ``libcpe_decode.so`` in-tree with hipcc.
 
 The kernel instantiations are split over several translation units
-(``csrc/launch_*.hip``) that are compiled in parallel, then linked with the
-host part (``csrc/cpe_decode.hip``) into one shared library.
+(``csrc/launch_*.hip``, ``csrc/head/*_*.hip``) that are compiled in parallel,
+then linked with the host parts (``csrc/cpe_decode.hip``, ``csrc/head/norm.hip``,
+``csrc/head/linear.hip``) into one shared library.
 """
 from __future__ import annotations
 
@@ -27,7 +28,7 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "head", "*.hip")))
 
 
 def build(verbose: bool = False, jobs: int = 8) -> str:

@@ -1,4 +1,4 @@
-// head_common.hpp -- element types, vector access and activations shared by
+// common.hpp -- element types, vector access and activations shared by
 // the head operators (group norm, linear).
 #pragma once
 
@@ -98,7 +98,7 @@ __device__ __forceinline__ int xcd_order(int w, int n)
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
-inline size_t element_size(cpe_dtype t) { return t == CPE_F32 ? 4 : 2; }
+inline size_t element_size(cpe_head_dtype t) { return t == CPE_HEAD_F32 ? 4 : 2; }
 inline size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace cpe

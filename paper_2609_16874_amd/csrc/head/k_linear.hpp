@@ -19,7 +19,7 @@
 // permuted by the bits of k that one read's lanes span.
 #pragma once
 
-#include "head_common.hpp"
+#include "common.hpp"
 #include "linear.hpp"
 
 #pragma clang fp contract(fast)
@@ -498,23 +498,36 @@ __global__ __launch_bounds__(256, 2) void k_gemm_narrow(GemmArgs g)
     // the first element of chunk c, and how many of its elements are not its own
     auto start = [&](int c) { return FULL || c * E <= g.k - E ? c * E : g.k - E; };
     auto extra = [&](int c) { return c * E - start(c); };
-    for (int q = threadIdx.x; q < n_pad * kRow; q += 256) {
-        int n, c;
-        T e[E];
-        if constexpr (B_ACROSS) {       // neighbouring threads read neighbouring n
-            c = q / n_pad;
-            n = q - c * n_pad;
-        } else {
-            n = q / kRow;
-            c = q - n * kRow;
-        }
-        const int k0 = start(c), skip = n < g.n ? extra(c) : E;
-        const T *p = static_cast<const T *>(g.b) + (B_ACROSS ? (int64_t)k0 * g.ldb + n : (int64_t)n * g.ldb + k0);
+    // B's chunks, kSetup of a thread's in flight at a time
+    constexpr int kSetup = 4;
+    for (int q0 = threadIdx.x; q0 < n_pad * kRow; q0 += kSetup * 256) {
+        T e[kSetup][E];
+        int place[kSetup];
 #pragma unroll
-        for (int i = 0; i < E; i++) e[i] = i >= skip ? p[B_ACROSS ? i * g.ldb : i] : (T)0.0f;
-        Fragment f;
-        __builtin_memcpy(&f, e, 16);
-        *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
+        for (int u = 0; u < kSetup; u++) {
+            const int q = q0 + u * 256;
+            // (across k neighbouring threads read neighbouring n)
+            const int n = B_ACROSS ? q % n_pad : q / kRow, c = B_ACROSS ? q / n_pad : q % kRow;
+            const bool on = q < n_pad * kRow && n < g.n;
+            const int k0 = start(c), skip = on ? extra(c) : E;
+            const T *p = static_cast<const T *>(g.b) + (B_ACROSS ? (int64_t)k0 * g.ldb + n : (int64_t)n * g.ldb + k0);
+            place[u] = q < n_pad * kRow ? (n * kRow + (c ^ narrow_swizzle(n))) * 16 : -1;
+            if constexpr (B_ACROSS) {
+#pragma unroll
+                for (int i = 0; i < E; i++) e[u][i] = i >= skip ? p[i * g.ldb] : (T)0.0f;
+            } else {
+                Vec<T, E> v;
+                if (on) v = load_vec<T, E>(p);
+#pragma unroll
+                for (int i = 0; i < E; i++) e[u][i] = i >= skip ? v.v[i] : (T)0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSetup; u++) {
+            Fragment f;
+            __builtin_memcpy(&f, e[u], 16);
+            if (place[u] >= 0) *(__attribute__((address_space(3))) u32x4 *)(lds + place[u]) = f.u;
+        }
     }
     const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
     const int row0 = (wave_base() >> 6) * 16 * MT;       // this wave's rows of a strip
@@ -1070,10 +1083,13 @@ int narrow_bytes(const GemmArgs &g)
 {
     return (int)(ceil_div(g.n, 32) * 32 * narrow_steps<T>(g.k) * 64);
 }
+// In f16, 200,000 rows: 256 to 64 34 us against 47 in tiles, 100 to 65 31 against
+// 49; with more columns the strips' epilogues outlast their loads (64 to 256 65
+// against 60, 128 to 256 96 against 70).
 template <typename T>
 bool narrow_fits(const GemmArgs &g)
 {
-    return g.k >= kChunk<T> && narrow_steps<T>(g.k) > 0 && g.n <= 4096 && narrow_bytes<T>(g) <= kNarrowLds;
+    return g.k >= kChunk<T> && narrow_steps<T>(g.k) > 0 && g.n <= 128 && narrow_bytes<T>(g) <= kNarrowLds;
 }
 
 template <typename T, bool B_ACROSS, int ACT>
@@ -1103,7 +1119,9 @@ hipError_t launch_narrow(const GemmArgs &g, hipStream_t stream)
 template <typename T, int ACT>
 hipError_t launch_forward(const GemmArgs &g, hipStream_t stream)
 {
-    if (g.m <= 64) return launch_rows<T, ACT>(g, stream);
+    // few rows: 10 us against 13 at 64 x 1024 to 1024; with more than 16 rows only
+    // while w stays in the caches (64 x 4096 to 4096: 23 us, in tiles 16)
+    if (g.m <= 16 || (g.m <= 64 && (int64_t)g.n * g.k <= (int64_t)1 << 22)) return launch_rows<T, ACT>(g, stream);
     if (narrow_fits<T>(g)) return launch_narrow<T, false, ACT>(g, stream);
     return launch_tiles<T, false, false, ACT>(g, stream);
 }

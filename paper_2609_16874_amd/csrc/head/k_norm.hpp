@@ -23,7 +23,7 @@
 // about it, less (sum (x - m))^2 / n for m's own rounding.
 #pragma once
 
-#include "head_common.hpp"
+#include "common.hpp"
 #include "norm.hpp"
 
 #pragma clang fp contract(fast)

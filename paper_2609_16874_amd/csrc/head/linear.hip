@@ -4,13 +4,13 @@
 
 #include <new>
 
-#include "head_common.hpp"
+#include "common.hpp"
 
 using namespace cpe;
 
 struct cpe_linear {
     int32_t max_rows, in, out;
-    cpe_dtype dtype;
+    cpe_head_dtype dtype;
     cpe_activation act;
     int device;
     unsigned char *ws;
@@ -35,54 +35,52 @@ cpe_status check_call(const cpe_linear *h, int32_t rows)
 
 hipError_t launch_gemm(const cpe_linear *h, const GemmArgs &g, hipStream_t stream)
 {
-    return h->dtype == CPE_F32   ? launch_gemm_f32(g, stream)
-           : h->dtype == CPE_F16 ? launch_gemm_f16(g, stream)
+    return h->dtype == CPE_HEAD_F32   ? launch_gemm_f32(g, stream)
+           : h->dtype == CPE_HEAD_F16 ? launch_gemm_f16(g, stream)
                                  : launch_gemm_bf16(g, stream);
 }
 
 hipError_t launch_grad(const cpe_linear *h, const GradArgs &g, hipStream_t stream)
 {
-    return h->dtype == CPE_F32   ? launch_grad_f32(g, stream)
-           : h->dtype == CPE_F16 ? launch_grad_f16(g, stream)
+    return h->dtype == CPE_HEAD_F32   ? launch_grad_f32(g, stream)
+           : h->dtype == CPE_HEAD_F16 ? launch_grad_f16(g, stream)
                                  : launch_grad_bf16(g, stream);
 }
 
-// The gradient in one pass: whole vectors of features, a dw that eight waves'
-// registers hold, and rows enough for every workgroup to have some.
-constexpr int kNarrowGradRows = 4096;
-
-}  // namespace
-
-namespace cpe {
+// The gradient in one pass: whole vectors of features and a dw that eight
+// waves' registers hold.  14.5 us against 24 .. 36 for the three products from
+// 100 to 4000 rows (64 to 256 features), 110 against 200 at 409,600.
 bool narrow_grad_fits(const WholeGradArgs &a)
 {
-    if (a.rows < kNarrowGradRows || a.n % 8 != 0 || a.k % 8 != 0) return false;
+    if (a.rows < 1 || a.n % 8 != 0 || a.k % 8 != 0) return false;
     return (a.n <= 128 && a.k <= 256) || (a.n <= 64 && a.k <= 512);
 }
+
 // Few rows: two launches instead of four or five, 14 us against 20 on small
 // products (calls as a program makes them).  Every workgroup forms the dz that
 // it needs again and gathers w's columns, which costs more than that on larger
 // ones: bf16 16 x 2048 to 4096 46 us against 33, 64 x 1024 to 1024 29 against
 // 27; binary32, whose tiles waste more on rows that are not there, 23 x 3776 to
 // 1152 28 against 39.
-bool rows_grad_fits(const WholeGradArgs &a, cpe_dtype dtype)
+bool rows_grad_fits(const WholeGradArgs &a, cpe_head_dtype dtype)
 {
-    const int64_t most = (int64_t)1 << (dtype == CPE_F32 ? 27 : 25);
+    const int64_t most = (int64_t)1 << (dtype == CPE_HEAD_F32 ? 27 : 25);
     return a.rows >= 1 && a.rows <= 64 && (int64_t)a.rows * a.n * a.k <= most;
 }
-}  // namespace cpe
+
+}  // namespace
 
 extern "C" {
 
 cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_features, int32_t out_features,
-                             cpe_dtype dtype, cpe_activation act)
+                             cpe_head_dtype dtype, cpe_activation act)
 {
     if (!out) return CPE_ERR_INVALID_ARG;
     *out = nullptr;
     if (max_rows < 1 || max_rows > 0x7fffffff - (1 << 23) + 1) return CPE_ERR_INVALID_ARG;
     if (in_features < 1 || in_features > 65536 || out_features < 1 || out_features > 65536)
         return CPE_ERR_INVALID_ARG;
-    if (dtype != CPE_F32 && dtype != CPE_F16 && dtype != CPE_BF16) return CPE_ERR_INVALID_ARG;
+    if (dtype != CPE_HEAD_F32 && dtype != CPE_HEAD_F16 && dtype != CPE_HEAD_BF16) return CPE_ERR_INVALID_ARG;
     if (act < CPE_ACT_NONE || act > CPE_ACT_GELU) return CPE_ERR_INVALID_ARG;
     cpe_linear *h = new (std::nothrow) cpe_linear{};
     if (!h) return CPE_ERR_OUT_OF_MEMORY;
@@ -188,13 +186,13 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
         a.k = h->in;
         a.act = h->act;
         if (rows_grad_fits(a, h->dtype)) {
-            const hipError_t e = h->dtype == CPE_F32   ? launch_rows_grad_f32(a, stream)
-                                 : h->dtype == CPE_F16 ? launch_rows_grad_f16(a, stream)
+            const hipError_t e = h->dtype == CPE_HEAD_F32   ? launch_rows_grad_f32(a, stream)
+                                 : h->dtype == CPE_HEAD_F16 ? launch_rows_grad_f16(a, stream)
                                                        : launch_rows_grad_bf16(a, stream);
             return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
         }
-        if (h->dtype != CPE_F32 && narrow_grad_fits(a)) {
-            const hipError_t e = h->dtype == CPE_F16 ? launch_narrow_grad_f16(a, stream)
+        if (h->dtype != CPE_HEAD_F32 && narrow_grad_fits(a)) {
+            const hipError_t e = h->dtype == CPE_HEAD_F16 ? launch_narrow_grad_f16(a, stream)
                                                      : launch_narrow_grad_bf16(a, stream);
             return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
         }

@@ -63,12 +63,10 @@ hipError_t launch_gemm_bf16(const GemmArgs &g, hipStream_t stream);
 hipError_t launch_grad_f32(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_f16(const GradArgs &g, hipStream_t stream);
 hipError_t launch_grad_bf16(const GradArgs &g, hipStream_t stream);
-// whether the gradient is done in one pass (16-bit types), and that pass
-bool narrow_grad_fits(const WholeGradArgs &a);
+// in one pass over the rows (16-bit types)
 hipError_t launch_narrow_grad_f16(WholeGradArgs a, hipStream_t stream);
 hipError_t launch_narrow_grad_bf16(WholeGradArgs a, hipStream_t stream);
-// whether there are few rows, and the gradient of those
-bool rows_grad_fits(const WholeGradArgs &a, cpe_dtype dtype);
+// of few rows
 hipError_t launch_rows_grad_f32(const WholeGradArgs &a, hipStream_t stream);
 hipError_t launch_rows_grad_f16(const WholeGradArgs &a, hipStream_t stream);
 hipError_t launch_rows_grad_bf16(const WholeGradArgs &a, hipStream_t stream);

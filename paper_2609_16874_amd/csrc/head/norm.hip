@@ -5,13 +5,13 @@
 #include <cmath>
 #include <new>
 
-#include "head_common.hpp"
+#include "common.hpp"
 
 using namespace cpe;
 
 struct cpe_norm {
     int32_t max_samples, max_pixels, channels, groups;
-    cpe_dtype dtype;
+    cpe_head_dtype dtype;
     cpe_activation act;
     float eps;
     int device;
@@ -50,8 +50,8 @@ cpe_status check_call(const cpe_norm *h, int32_t samples, int32_t pixels, const 
 cpe_status launch(const cpe_norm *h, const NormArgs &a, hipStream_t stream)
 {
     (void)hipGetLastError();
-    const hipError_t e = h->dtype == CPE_F32   ? launch_norm_f32(a, stream)
-                         : h->dtype == CPE_F16 ? launch_norm_f16(a, stream)
+    const hipError_t e = h->dtype == CPE_HEAD_F32   ? launch_norm_f32(a, stream)
+                         : h->dtype == CPE_HEAD_F16 ? launch_norm_f16(a, stream)
                                                : launch_norm_bf16(a, stream);
     return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
 }
@@ -82,7 +82,7 @@ NormArgs common_args(const cpe_norm *h, int32_t samples, int32_t pixels, const f
 extern "C" {
 
 cpe_status cpe_norm_create(cpe_norm **out, int32_t max_samples, int32_t max_pixels, int32_t channels,
-                           int32_t groups, cpe_dtype dtype, cpe_activation act, float eps)
+                           int32_t groups, cpe_head_dtype dtype, cpe_activation act, float eps)
 {
     if (!out) return CPE_ERR_INVALID_ARG;
     *out = nullptr;
@@ -90,7 +90,7 @@ cpe_status cpe_norm_create(cpe_norm **out, int32_t max_samples, int32_t max_pixe
         return CPE_ERR_INVALID_ARG;
     if (channels < 1 || channels > kNormMaxChannels || groups < 1 || channels % groups != 0)
         return CPE_ERR_INVALID_ARG;
-    if (dtype != CPE_F32 && dtype != CPE_F16 && dtype != CPE_BF16) return CPE_ERR_INVALID_ARG;
+    if (dtype != CPE_HEAD_F32 && dtype != CPE_HEAD_F16 && dtype != CPE_HEAD_BF16) return CPE_ERR_INVALID_ARG;
     if (act < CPE_ACT_NONE || act > CPE_ACT_GELU) return CPE_ERR_INVALID_ARG;
     if (!std::isfinite(eps) || eps <= 0.0f) return CPE_ERR_INVALID_ARG;
     cpe_norm *h = new (std::nothrow) cpe_norm{};

@@ -15,9 +15,9 @@ from typing import Optional
 
 import torch
 
-from .native import CPE_BF16, CPE_F16, CPE_F32, CPE_OK, CpeError, library, torch_dtype
+from .native import CPE_OK, CpeError, library, torch_dtype
 
-DTYPES = {"f32": CPE_F32, "f16": CPE_F16, "bf16": CPE_BF16}
+DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 

@@ -51,7 +51,7 @@ def test_null_handles():
 def test_the_decoder_takes_no_bf16():
     import numpy as np
     h, f = _handle(), np.ones(4)
-    assert native.library().cpe_decode_create(ctypes.byref(h), 16, 16, 16, native.CPE_BF16, f.ctypes.data,
+    assert native.library().cpe_decode_create(ctypes.byref(h), 16, 16, 16, 2, f.ctypes.data,
                                               f.ctypes.data, 4, 8, 8, 16) == native.CPE_ERR_INVALID_ARG
 
 
