@@ -1029,6 +1029,8 @@ void choose_splits(GemmArgs &g)
         splits = kSplitTiles / 2 / tiles;
         if (splits > steps / kLeast) splits = steps / kLeast;
     }
+    const int64_t one = (int64_t)g.m * ceil_div(g.n, 4) * 16;      // a split's partial outputs, in the scratch
+    if (splits > kSplitBytes / one) splits = kSplitBytes / one;
     if (splits < 1) splits = 1;
     const int64_t each = ceil_div(steps, splits);
     g.k_split = (int32_t)(each * kStepK<T>);

@@ -94,7 +94,7 @@ cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_feat
         return CPE_ERR_HIP;
     }
     h->dz_ld = (out_features + 7) / 8 * 8;
-    h->sums_at = align256((size_t)kSplitTiles * kTile * kTile * 4);
+    h->sums_at = align256((size_t)kSplitBytes);
     h->dz_at = h->sums_at + align256((size_t)kSumBlocks * (out_features < 2048 ? out_features : 2048) * 4);
     h->ws_bytes = h->dz_at;
     if (act != CPE_ACT_NONE) h->ws_bytes += align256((size_t)max_rows * h->dz_ld * element_size(dtype));

@@ -11,7 +11,8 @@ namespace cpe {
 
 constexpr int kGemmThreads = 256;
 constexpr int kTile = 128;                    // output rows and columns of a workgroup
-constexpr int kSplitTiles = 512;              // partial tiles of a split product (its scratch)
+constexpr int kSplitTiles = 512;              // partial tiles of a split product
+constexpr int64_t kSplitBytes = (int64_t)kSplitTiles * kTile * kTile * 4;       // and their scratch
 constexpr int64_t kMaxTiles = (int64_t)1 << 22;
 constexpr int kSumBlocks = 1024;              // workgroups along the rows of the bias gradient
 

@@ -21,6 +21,7 @@ SHAPES = [
     (257, 520, 136, 24), (1000, 64, 200, 0), (100, 4096, 96, 0), (90, 2049, 130, 0), (5000, 24, 8, 0),
     (12345, 48, 40, 0), (4100, 256, 128, 0), (4097, 512, 64, 8), (6001, 200, 120, 0), (9000, 136, 16, 5), (5000, 304, 40, 0),
     (2, 520, 1032, 0), (33, 130, 70, 5), (64, 1000, 264, 0), (48, 96, 2500, 0),
+    (2050, 2072, 2056, 0), (4100, 136, 4104, 8),
 ]
 
 
