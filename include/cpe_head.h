@@ -25,7 +25,7 @@
  * The handle owns the scratch, allocated at create and freed at destroy; the
  * calls themselves never allocate, never synchronise and never copy to the
  * host: they enqueue work on `stream`.  Nothing is kept from one call for the
- * next, and results do not vary from run to run (no atomics).
+ * next, and results do not vary from run to run (sums have a fixed order).
  *
  * Errors.  Argument errors are found on the host before any work is enqueued
  * and return CPE_ERR_INVALID_ARG; a failed launch returns CPE_ERR_HIP (the

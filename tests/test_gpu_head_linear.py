@@ -148,6 +148,30 @@ def test_no_rows_and_single_outputs():
     h.close()
 
 
+@pytest.mark.parametrize("N", [24, 136])
+def test_pointers_off_16_bytes(N):
+    """Rows that start one element into their buffers."""
+    M, K = 300, 72
+    h = head().Linear(M, K, N, "f16", "relu")
+    x, w, dy, z = (matrix(a, b, "f16", 40 + i) for i, (a, b) in enumerate(((M, K), (N, K), (M, N), (M, N))))
+
+    def off(m):
+        full = torch.full((m.shape[0], m.shape[1] + 1), float("nan"), dtype=m.dtype, device="cuda")
+        full[:, 1:] = m.cuda()
+        return full[:, 1:]
+
+    y = h.run(x.cuda(), w.cuda())
+    other = torch.full((M, N + 1), 77.0, dtype=torch.float16, device="cuda")
+    assert h.forward(off(x), off(w), None, other[:, 1:]) == 0
+    # (the two may add up in other orders: a unit of the sums' rounding apart)
+    assert float((other[:, 1:].float() - y.float()).abs().max()) <= 2.0 ** -10 * float(y.abs().max())
+    assert bool((other[:, 0] == 77.0).all())
+    for a, b in zip(h.run_backward(x.cuda(), w.cuda(), dy.cuda(), z.cuda()),
+                    h.run_backward(off(x), off(w), off(dy), off(z))):
+        assert float((a.float() - b.float()).abs().max()) <= 2.0 ** -10 * float(a.abs().max())
+    h.close()
+
+
 def test_residual_in_place_and_infinities():
     x, w, res = matrix(100, 64, "f16", 1), matrix(32, 64, "f16", 2, 0.125), matrix(100, 32, "f16", 3)
     h = head().Linear(100, 64, 32, "f16", "gelu")
@@ -208,10 +232,11 @@ def test_runs_repeat_and_streams_and_graphs():
         h.close()
 
 
-def test_offsets_beyond_32_bits():
+@pytest.mark.parametrize("N", [16, 136])
+def test_offsets_beyond_32_bits(N):
     """2,200,000 rows of 1024 features: 2.25e9 elements; equal rows far apart
-    give equal outputs."""
-    M, K, N = 2_200_000, 1024, 16
+    give equal outputs (narrow and tiled products)."""
+    M, K = 2_200_000, 1024
     n = M // 10
     g = torch.Generator(device="cuda").manual_seed(1)
     part = torch.randn((n, K), generator=g, device="cuda").to(torch.bfloat16)

@@ -243,6 +243,32 @@ def test_other_orders_views_and_in_place():
     h.close()
 
 
+@pytest.mark.parametrize("C,P", [(64, 3000), (50, 3000), (32, 100)])
+def test_pointers_off_16_bytes_and_large_maps_in_place(C, P):
+    """Maps that start one element into their buffers give the same."""
+    G = 2
+    x, gamma, beta, _, real = inputs((2, P, C, G, 0, None), "f16", seed=8)
+    dy = make(2, P, C, 0, "f16", 9).cuda()
+    h = head().GroupNorm(2, P, C, G, "f16", "silu", EPS)
+    y, stats = h.run(x.cuda(), gamma.cuda(), beta.cuda())
+
+    def off(t):
+        full = torch.full(t.shape[:-1] + (C + 1,), 77.0, dtype=t.dtype, device="cuda")
+        full[..., 1:] = t
+        return full
+
+    place = off(x.cuda())
+    assert h.forward(place[..., 1:], gamma.cuda(), beta.cuda(), place[..., 1:]) == 0
+    assert torch.equal(place[..., 1:], y) and bool((place[..., 0] == 77.0).all())
+    dx, dg, db = h.run_backward(x.cuda(), dy, gamma.cuda(), beta.cuda(), stats)
+    place = off(dy)
+    dg2, db2 = torch.empty_like(dg), torch.empty_like(db)
+    assert h.backward(off(x.cuda())[..., 1:], place[..., 1:], gamma.cuda(), beta.cuda(), stats, place[..., 1:], dg2,
+                      db2) == 0
+    assert torch.equal(place[..., 1:], dx) and torch.equal(dg, dg2) and torch.equal(db, db2)
+    h.close()
+
+
 def test_nothing_to_do():
     h = head().GroupNorm(2, 10, 8, 2, "f32")
     gamma = torch.ones(8, device="cuda")
