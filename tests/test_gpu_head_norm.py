@@ -33,6 +33,7 @@ SHAPES = [
     (3, 40, 24, 2, 1, (-3, 17, 39)),
     (1, 70001, 16, 2, 0, None),
     (70, 11, 32, 4, 0, None),
+    (90, 11, 32, 8, 0, None),                  # more groups than workgroups at once
     (2, 20011, 125, 25, 0, None),              # 16-byte vectors that end across the row's end
     (1, 30001, 13, 13, 2, (29000,)),
     (1, 9001, 2053, 1, 0, None),
