@@ -7,9 +7,14 @@ their pointers, strides and torch's current HIP stream are passed through.
 Calls return the C ABI's status; ``native.CpeError`` is raised by the
 constructors and by the ``run`` conveniences.  A tensor whose shape, dtype or
 device the C ABI could not see is refused here with ``ValueError``.
+
+``stream`` stands for ``with torch.cuda.stream(stream)`` around the call: what
+``run`` and ``run_backward`` allocate belongs to it.  Inputs that another
+stream writes, and outputs that another stream reads, are ordered by the caller.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import Optional
 
@@ -25,6 +30,12 @@ def _stream(stream, device: int) -> int:
     """The HIP stream's handle (the current one's without the stream object,
     whose construction takes as long as the launch)."""
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _allocating(stream):
+    """New tensors are taken from the pool of the stream that writes them: a
+    block of the current stream's pool may have work on it that is still to run."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _need(ok: bool, what: str):
@@ -102,8 +113,9 @@ class GroupNorm:
 
     def run(self, x, gamma, beta, valid=None, stream=None):
         """forward into new tensors: (y, stats)."""
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        stats = torch.empty((x.shape[0], self.groups, 2), dtype=torch.float32, device=x.device)
+        with _allocating(stream):
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            stats = torch.empty((x.shape[0], self.groups, 2), dtype=torch.float32, device=x.device)
         st = self.forward(x, gamma, beta, y, stats, valid, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_forward")
@@ -111,8 +123,9 @@ class GroupNorm:
 
     def run_backward(self, x, dy, gamma, beta, stats, valid=None, stream=None):
         """backward into new tensors: (dx, dgamma, dbeta)."""
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dgamma, dbeta = (torch.empty(self.channels, dtype=torch.float32, device=x.device) for _ in range(2))
+        with _allocating(stream):
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dgamma, dbeta = (torch.empty(self.channels, dtype=torch.float32, device=x.device) for _ in range(2))
         st = self.backward(x, dy, gamma, beta, stats, dx, dgamma, dbeta, valid, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_backward")
@@ -185,8 +198,9 @@ class Linear:
 
     def run(self, x, weight, bias=None, residual=None, keep=False, stream=None):
         """forward into new tensors: y, or (y, preact) where ``keep``."""
-        y = torch.empty((x.shape[0], self.out_features), dtype=x.dtype, device=x.device)
-        preact = torch.empty_like(y) if keep else None
+        with _allocating(stream):
+            y = torch.empty((x.shape[0], self.out_features), dtype=x.dtype, device=x.device)
+            preact = torch.empty_like(y) if keep else None
         st = self.forward(x, weight, bias, y, residual, preact, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_linear_forward")
@@ -194,9 +208,10 @@ class Linear:
 
     def run_backward(self, x, weight, dy, preact=None, stream=None):
         """backward into new tensors: (dx, dweight, dbias)."""
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dweight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
-        dbias = torch.empty(self.out_features, dtype=torch.float32, device=x.device)
+        with _allocating(stream):
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dweight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
+            dbias = torch.empty(self.out_features, dtype=torch.float32, device=x.device)
         st = self.backward(x, weight, dy, preact, dx, dweight, dbias, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_linear_backward")

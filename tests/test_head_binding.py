@@ -1,0 +1,142 @@
+"""What the binding of the head operators does before the C ABI is called:
+where it allocates, and which tensors and sizes it refuses.  The CPU tests
+stand a recorder in the library's place."""
+import contextlib
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+class Recorder:
+    """A library whose entry points note their arguments and return CPE_OK."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+class Tensor:
+    """The attributes of a device tensor that the binding looks at."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype=torch.float16, strides=None, device=0, pointer=4096):
+        self.shape, self.dtype, self._device, self._pointer = tuple(shape), dtype, device, pointer
+        if strides is None:
+            strides, step = [], 1
+            for n in reversed(self.shape):
+                strides.insert(0, step)
+                step *= max(1, n)
+        self._strides = tuple(strides)
+        self.device = torch.device("cuda", device)
+        self.requires_grad = False
+
+    def stride(self):
+        return self._strides
+
+    def data_ptr(self):
+        return self._pointer
+
+    def get_device(self):
+        return self._device
+
+    def numel(self):
+        n = 1
+        for s in self.shape:
+            n *= s
+        return n
+
+    def is_contiguous(self):
+        return True
+
+
+class Stream:
+    cuda_stream = 77
+
+
+def norm(channels=8, groups=2):
+    from paper_2609_16874_amd import head
+    h = object.__new__(head.GroupNorm)
+    h.channels, h.groups, h.dtype, h.eps = channels, groups, "f16", 1e-5
+    h._torch_dtype, h._lib, h._h, h._device = torch.float16, Recorder(), 123, 0
+    return h
+
+
+def linear(k=8, n=6):
+    from paper_2609_16874_amd import head
+    h = object.__new__(head.Linear)
+    h.in_features, h.out_features, h.dtype = k, n, "f16"
+    h._torch_dtype, h._lib, h._h, h._device = torch.float16, Recorder(), 123, 0
+    return h
+
+
+def _runs(stream):
+    """The four conveniences, each on its own handle."""
+    x, m, w = Tensor((2, 4, 8)), Tensor((4, 8)), Tensor((6, 8))
+    dm, stats = Tensor((4, 6)), Tensor((2, 2, 2), torch.float32)
+    return {"norm": lambda: norm().run(x, None, None, stream=stream),
+            "norm backward": lambda: norm().run_backward(x, x, None, None, stats, stream=stream),
+            "linear": lambda: linear().run(m, w, keep=True, stream=stream),
+            "linear backward": lambda: linear().run_backward(m, w, dm, dm, stream=stream)}
+
+
+@pytest.mark.parametrize("which", ["norm", "norm backward", "linear", "linear backward"])
+@pytest.mark.parametrize("given", [True, False])
+def test_outputs_are_allocated_on_the_stream_that_writes_them(which, given, monkeypatch):
+    from paper_2609_16874_amd import head
+    inside, streams = [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        streams.append(stream)
+        yield
+        streams.pop()
+
+    def empty(shape, dtype=None, device=None):
+        inside.append(streams[-1] if streams else None)
+        return Tensor((shape,) if isinstance(shape, int) else shape, dtype)
+
+    monkeypatch.setattr(head.torch.cuda, "stream", on)
+    monkeypatch.setattr(head.torch, "empty", empty)
+    monkeypatch.setattr(head.torch, "empty_like", lambda t: empty(t.shape, t.dtype))
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0 if stream is None else stream.cuda_stream)
+    stream = Stream() if given else None
+    _runs(stream)[which]()
+    assert len(inside) >= 2 and all(s is stream for s in inside)
+
+
+@pytest.mark.gpu
+def test_outputs_do_not_take_memory_that_pending_work_still_uses():
+    """A block freed on the current stream while a fill of it waits there
+    behind other work: a run on a side stream must not write its output there."""
+    from paper_2609_16874_amd import head
+    M, K, N = 4096, 256, 256
+    g = torch.Generator().manual_seed(1)
+    x, w = (torch.randn(s, generator=g).half().cuda() for s in ((M, K), (N, K)))
+    h = head.Linear(M, K, N, "f16")
+    n = head.GroupNorm(1, M, K, 8, "f16")
+    want = h.run(x, w)
+    want_n, _ = n.run(x[None], None, None)
+    side = torch.cuda.Stream()
+    a = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        blocks = [torch.empty_like(want) for _ in range(2)] + [torch.empty_like(want_n)]
+        for _ in range(8):
+            b = a @ a           # the current stream is busy
+        for t in blocks:
+            t.fill_(7.0)
+        del blocks, t
+        got = h.run(x, w, stream=side)
+        got_n, _ = n.run(x[None], None, None, stream=side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(got_n, want_n)
+    del b
+    h.close()
+    n.close()
