@@ -43,12 +43,12 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _vector(t, n: int, name: str, dtype=torch.float32):
+def _vector(t, n: int, name: str, device: int, dtype=torch.float32):
     """The pointer of a contiguous device vector, or None."""
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype is dtype and t.numel() == n and t.is_contiguous()):
-        raise ValueError(f"{name}: a contiguous device tensor of {n} {dtype} is needed")
+    if not (t.is_cuda and t.get_device() == device and t.dtype is dtype and t.numel() == n and t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous tensor of {n} {dtype} on the handle's device is needed")
     return t.data_ptr()
 
 
@@ -82,8 +82,9 @@ class GroupNorm:
             _need(height <= 1 or width == 0 or strides[1] == width * strides[2],
                   f"{name}: image rows must follow one another")
             ld = strides[2] if width > 1 else strides[1]
-        if not (t.is_cuda and t.dtype is self._torch_dtype and channels == self.channels
-                and (channels == 1 or strides[-1] == 1) and (size is None or size == (samples, pixels))):
+        if not (t.is_cuda and t.get_device() == self._device and t.dtype is self._torch_dtype
+                and channels == self.channels and (channels == 1 or strides[-1] == 1)
+                and (size is None or size == (samples, pixels))):
             raise ValueError(f"{name}: wrong shape, dtype, device or channel stride")
         if pixels <= 1 and ld < channels:      # the stride of a single pixel says nothing
             ld = channels
@@ -94,22 +95,25 @@ class GroupNorm:
         gradient; ``valid`` holds int32 pixel counts, one per sample."""
         px, x_ld, x_sample, size = self._map(x, "x")
         py, y_ld, y_sample, _ = self._map(y, "y", size)
+        dev = self._device
         return self._lib.cpe_norm_forward(
-            self._h, _stream(stream, self._device), size[0], size[1], px, x_ld, x_sample,
-            _vector(gamma, self.channels, "gamma"), _vector(beta, self.channels, "beta"),
-            _vector(valid, size[0], "valid", torch.int32), py, y_ld, y_sample,
-            _vector(stats, 2 * size[0] * self.groups, "stats"))
+            self._h, _stream(stream, dev), size[0], size[1], px, x_ld, x_sample,
+            _vector(gamma, self.channels, "gamma", dev), _vector(beta, self.channels, "beta", dev),
+            _vector(valid, size[0], "valid", dev, torch.int32), py, y_ld, y_sample,
+            _vector(stats, 2 * size[0] * self.groups, "stats", dev))
 
     def backward(self, x, dy, gamma, beta, stats, dx=None, dgamma=None, dbeta=None, valid=None, stream=None) -> int:
         """cpe_norm_backward: writes those of dx, dgamma and dbeta that are given."""
         px, x_ld, x_sample, size = self._map(x, "x")
         pd, dy_ld, dy_sample, _ = self._map(dy, "dy", size)
         po, dx_ld, dx_sample, _ = (None, 0, 0, None) if dx is None else self._map(dx, "dx", size)
+        dev = self._device
         return self._lib.cpe_norm_backward(
-            self._h, _stream(stream, self._device), size[0], size[1], px, x_ld, x_sample, pd, dy_ld, dy_sample,
-            _vector(gamma, self.channels, "gamma"), _vector(beta, self.channels, "beta"),
-            _vector(valid, size[0], "valid", torch.int32), _vector(stats, 2 * size[0] * self.groups, "stats"),
-            po, dx_ld, dx_sample, _vector(dgamma, self.channels, "dgamma"), _vector(dbeta, self.channels, "dbeta"))
+            self._h, _stream(stream, dev), size[0], size[1], px, x_ld, x_sample, pd, dy_ld, dy_sample,
+            _vector(gamma, self.channels, "gamma", dev), _vector(beta, self.channels, "beta", dev),
+            _vector(valid, size[0], "valid", dev, torch.int32),
+            _vector(stats, 2 * size[0] * self.groups, "stats", dev), po, dx_ld, dx_sample,
+            _vector(dgamma, self.channels, "dgamma", dev), _vector(dbeta, self.channels, "dbeta", dev))
 
     def run(self, x, gamma, beta, valid=None, stream=None):
         """forward into new tensors: (y, stats)."""
@@ -166,8 +170,8 @@ class Linear:
         if t is None:
             return None, 0
         shape, strides = t.shape, t.stride()
-        if not (len(shape) == 2 and t.is_cuda and t.dtype is self._torch_dtype and shape[1] == width
-                and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
+        if not (len(shape) == 2 and t.is_cuda and t.get_device() == self._device and t.dtype is self._torch_dtype
+                and shape[1] == width and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
             raise ValueError(f"{name}: wrong shape, dtype, device or feature stride")
         ld = strides[0]
         return t.data_ptr(), width if shape[0] <= 1 and ld < width else ld
@@ -182,7 +186,7 @@ class Linear:
         pr, r_ld = self._matrix(residual, rows, n, "residual")
         pz, z_ld = self._matrix(preact, rows, n, "preact")
         return self._lib.cpe_linear_forward(self._h, _stream(stream, self._device), rows, px, x_ld, pw, w_ld,
-                                            _vector(bias, n, "bias"), pr, r_ld, py, y_ld, pz, z_ld)
+                                            _vector(bias, n, "bias", self._device), pr, r_ld, py, y_ld, pz, z_ld)
 
     def backward(self, x, weight, dy, preact=None, dx=None, dweight=None, dbias=None, stream=None) -> int:
         """cpe_linear_backward: writes those of dx, dweight and dbias that are given."""
@@ -194,7 +198,8 @@ class Linear:
         po, o_ld = self._matrix(dx, rows, k, "dx")
         pg, g_ld = self._matrix(dweight, n, k, "dweight")
         return self._lib.cpe_linear_backward(self._h, _stream(stream, self._device), rows, px, x_ld, pw, w_ld, pd, d_ld,
-                                             pz, z_ld, po, o_ld, pg, g_ld, _vector(dbias, n, "dbias"))
+                                             pz, z_ld, po, o_ld, pg, g_ld,
+                                             _vector(dbias, n, "dbias", self._device))
 
     def run(self, x, weight, bias=None, residual=None, keep=False, stream=None):
         """forward into new tensors: y, or (y, preact) where ``keep``."""

@@ -140,3 +140,40 @@ def test_outputs_do_not_take_memory_that_pending_work_still_uses():
     del b
     h.close()
     n.close()
+
+
+@pytest.mark.parametrize("far", ["x", "gamma", "beta", "y", "stats", "valid"])
+def test_norm_tensors_of_another_device(far, monkeypatch):
+    from paper_2609_16874_amd import head
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
+    h = norm()
+    a = {"x": Tensor((2, 4, 8)), "gamma": Tensor((8,), torch.float32), "beta": Tensor((8,), torch.float32),
+         "y": Tensor((2, 4, 8)), "stats": Tensor((2, 2, 2), torch.float32), "valid": Tensor((2,), torch.int32)}
+    assert h.forward(**a) == 0 and len(h._lib.calls) == 1
+    a[far] = Tensor(a[far].shape, a[far].dtype, device=1)
+    with pytest.raises(ValueError):
+        h.forward(**a)
+    if far != "y":
+        b = {**a, "dy": Tensor((2, 4, 8)), "dx": Tensor((2, 4, 8))}
+        del b["y"]
+        with pytest.raises(ValueError):
+            h.backward(**b)
+    assert len(h._lib.calls) == 1
+
+
+@pytest.mark.parametrize("far", ["x", "weight", "dy", "preact", "dx", "dweight", "dbias", "bias", "residual"])
+def test_linear_tensors_of_another_device(far, monkeypatch):
+    from paper_2609_16874_amd import head
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
+    h = linear()
+    f = {"x": Tensor((4, 8)), "weight": Tensor((6, 8)), "bias": Tensor((6,), torch.float32), "y": Tensor((4, 6)),
+         "residual": Tensor((4, 6)), "preact": Tensor((4, 6))}
+    b = {"x": Tensor((4, 8)), "weight": Tensor((6, 8)), "dy": Tensor((4, 6)), "preact": Tensor((4, 6)),
+         "dx": Tensor((4, 8)), "dweight": Tensor((6, 8)), "dbias": Tensor((6,), torch.float32)}
+    assert h.forward(**f) == 0 and h.backward(**b) == 0 and len(h._lib.calls) == 2
+    for call, a in ((h.forward, f), (h.backward, b)):
+        if far in a:
+            a[far] = Tensor(a[far].shape, a[far].dtype, device=1)
+            with pytest.raises(ValueError):
+                call(**a)
+    assert len(h._lib.calls) == 2
