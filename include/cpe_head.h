@@ -118,6 +118,7 @@ cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_feat
  *   bias        device [N] float or NULL
  *   residual    device [rows][N] or NULL; may be y itself with the same stride
  *   preact      device [rows][N] or NULL: receives z for the gradient
+ * Apart from that residual, y and preact overlap no input and not each other.
  */
 cpe_status cpe_linear_forward(cpe_linear *h, hipStream_t stream, int32_t rows, const void *x, int64_t x_ld,
                               const void *w, int64_t w_ld, const float *bias, const void *residual,

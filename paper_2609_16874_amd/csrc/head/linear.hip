@@ -119,9 +119,11 @@ cpe_status cpe_linear_forward(cpe_linear *h, hipStream_t stream, int32_t rows, c
     if (rows == 0) return CPE_OK;
     if (!check_matrix(h, x, x_ld, h->in) || !check_matrix(h, w, w_ld, h->in) || !check_matrix(h, y, y_ld, h->out))
         return CPE_ERR_INVALID_ARG;
+    if (y == x || y == w) return CPE_ERR_INVALID_ARG;       // (other workgroups still read them)
     if (residual && !check_matrix(h, residual, residual_ld, h->out)) return CPE_ERR_INVALID_ARG;
     if (residual == y && residual_ld != y_ld) return CPE_ERR_INVALID_ARG;
-    if (preact && (!check_matrix(h, preact, preact_ld, h->out) || preact == y || preact == residual))
+    if (preact && (!check_matrix(h, preact, preact_ld, h->out) || preact == y || preact == residual || preact == x ||
+                   preact == w))
         return CPE_ERR_INVALID_ARG;
     GemmArgs g{};
     g.a = x;

@@ -139,3 +139,15 @@ def test_binding_refuses_what_the_abi_cannot_see():
         n.forward(x[0, 0], None, None, x)
     with pytest.raises(ValueError):
         lin.forward(x[0], x[0, :6], None, x[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("change", [dict(y=4096), dict(y=8192), dict(preact=4096, preact_ld=8),
+                                    dict(preact=8192, preact_ld=8), dict(preact=12288, preact_ld=8),
+                                    dict(preact=16384, preact_ld=8, residual=16384, residual_ld=8)])
+def test_linear_forward_refuses_outputs_in_place_of_inputs(change):
+    """Equal features, so that the shapes alone would allow it."""
+    lib, h = native.library(), ctypes.c_void_p()
+    assert lib.cpe_linear_create(ctypes.byref(h), 4, 8, 8, 1, 0) == 0
+    assert _linear_call(h, lib, y_ld=8, **change) == native.CPE_ERR_INVALID_ARG
+    assert lib.cpe_linear_destroy(h) == 0
