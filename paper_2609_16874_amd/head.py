@@ -43,6 +43,13 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _int32(v, what: str) -> int:
+    """A size as the C ABI's int32, which ctypes would cut off without a word."""
+    v = int(v)
+    _need(-(1 << 31) <= v < 1 << 31, f"{what}: {v} is no 32-bit size")
+    return v
+
+
 def _vector(t, n: int, name: str, device: int, dtype=torch.float32):
     """The pointer of a contiguous device vector, or None."""
     if t is None:
@@ -60,11 +67,12 @@ class GroupNorm:
 
     def __init__(self, max_samples: int, max_pixels: int, channels: int, groups: int, dtype: str,
                  activation: str = "none", eps: float = 1e-5):
-        self.channels, self.groups, self.dtype = int(channels), int(groups), dtype
+        self.channels, self.groups, self.dtype = _int32(channels, "channels"), _int32(groups, "groups"), dtype
         self._torch_dtype, self._lib = torch_dtype(dtype), library()
         h = ctypes.c_void_p()
-        st = self._lib.cpe_norm_create(ctypes.byref(h), int(max_samples), int(max_pixels), self.channels,
-                                       self.groups, DTYPES[dtype], ACTIVATIONS[activation], float(eps))
+        st = self._lib.cpe_norm_create(ctypes.byref(h), _int32(max_samples, "max_samples"),
+                                       _int32(max_pixels, "max_pixels"), self.channels, self.groups,
+                                       DTYPES[dtype], ACTIVATIONS[activation], float(eps))
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_create")
         self._h, self._device = h, torch.cuda.current_device()
@@ -88,6 +96,8 @@ class GroupNorm:
             raise ValueError(f"{name}: wrong shape, dtype, device or channel stride")
         if pixels <= 1 and ld < channels:      # the stride of a single pixel says nothing
             ld = channels
+        if size is None:
+            samples, pixels = _int32(samples, name), _int32(pixels, name)
         return t.data_ptr(), ld, strides[0], (samples, pixels)
 
     def forward(self, x, gamma, beta, y, stats=None, valid=None, stream=None) -> int:
@@ -156,11 +166,12 @@ class Linear:
     contiguous features and any row stride; the weight is [out][in]."""
 
     def __init__(self, max_rows: int, in_features: int, out_features: int, dtype: str, activation: str = "none"):
-        self.in_features, self.out_features, self.dtype = int(in_features), int(out_features), dtype
+        self.in_features, self.out_features = _int32(in_features, "in_features"), _int32(out_features, "out_features")
+        self.dtype = dtype
         self._torch_dtype, self._lib = torch_dtype(dtype), library()
         h = ctypes.c_void_p()
-        st = self._lib.cpe_linear_create(ctypes.byref(h), int(max_rows), self.in_features, self.out_features,
-                                         DTYPES[dtype], ACTIVATIONS[activation])
+        st = self._lib.cpe_linear_create(ctypes.byref(h), _int32(max_rows, "max_rows"), self.in_features,
+                                         self.out_features, DTYPES[dtype], ACTIVATIONS[activation])
         if st != CPE_OK:
             raise CpeError(st, "cpe_linear_create")
         self._h, self._device = h, torch.cuda.current_device()
@@ -179,7 +190,7 @@ class Linear:
     def forward(self, x, weight, bias, y, residual=None, preact=None, stream=None) -> int:
         """cpe_linear_forward: ``preact`` receives the value before the
         activation, which the gradient needs."""
-        rows, n = x.shape[0], self.out_features
+        rows, n = _int32(x.shape[0], "rows"), self.out_features
         px, x_ld = self._matrix(x, None, self.in_features, "x")
         pw, w_ld = self._matrix(weight, n, self.in_features, "weight")
         py, y_ld = self._matrix(y, rows, n, "y")
@@ -190,7 +201,7 @@ class Linear:
 
     def backward(self, x, weight, dy, preact=None, dx=None, dweight=None, dbias=None, stream=None) -> int:
         """cpe_linear_backward: writes those of dx, dweight and dbias that are given."""
-        rows, k, n = x.shape[0], self.in_features, self.out_features
+        rows, k, n = _int32(x.shape[0], "rows"), self.in_features, self.out_features
         px, x_ld = self._matrix(x, None, k, "x")
         pw, w_ld = self._matrix(weight, n, k, "weight")
         pd, d_ld = self._matrix(dy, rows, n, "dy")

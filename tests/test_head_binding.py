@@ -177,3 +177,35 @@ def test_linear_tensors_of_another_device(far, monkeypatch):
             with pytest.raises(ValueError):
                 call(**a)
     assert len(h._lib.calls) == 2
+
+
+WIDE = 2 ** 32 + 4      # 4, cut off to 32 bits
+
+
+@pytest.mark.parametrize("at", range(4))
+def test_sizes_of_handles_beyond_32_bits(at):
+    from paper_2609_16874_amd import head
+    for cls, sizes in ((head.GroupNorm, [4, 4, 4, 4]), (head.Linear, [4, 4, 4])):
+        if at < len(sizes):
+            sizes[at] = WIDE
+            with pytest.raises(ValueError):
+                cls(*sizes, "f16")
+
+
+def test_sizes_of_calls_beyond_32_bits(monkeypatch):
+    """A matrix of 2^32 + 4 rows is not one of four."""
+    from paper_2609_16874_amd import head
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
+    h, n = linear(1, 1), norm()
+    m, w = Tensor((WIDE, 1)), Tensor((1, 1))
+    with pytest.raises(ValueError):
+        h.forward(m, w, None, m)
+    with pytest.raises(ValueError):
+        h.backward(m, w, m, dx=m)
+    for shape in ((WIDE, 1, 8), (1, WIDE, 8), (1, 2 ** 16, 2 ** 16, 8)):
+        t = Tensor(shape)
+        with pytest.raises(ValueError):
+            n.forward(t, None, None, t)
+        with pytest.raises(ValueError):
+            n.backward(t, t, None, None, Tensor((2 * 2 * shape[0],), torch.float32), t)
+    assert not h._lib.calls and not n._lib.calls
