@@ -87,7 +87,8 @@ class GroupNorm:
             _need(len(shape) == 4, f"{name}: three or four dimensions, channels last")
             samples, height, width, channels = shape
             pixels = height * width
-            _need(height <= 1 or width == 0 or strides[1] == width * strides[2],
+            # (the stride of a dimension of one says nothing: a column's pixels are its image rows)
+            _need(height <= 1 or width <= 1 or strides[1] == width * strides[2],
                   f"{name}: image rows must follow one another")
             ld = strides[2] if width > 1 else strides[1]
         if not (t.is_cuda and t.get_device() == self._device and t.dtype is self._torch_dtype

@@ -209,3 +209,30 @@ def test_sizes_of_calls_beyond_32_bits(monkeypatch):
         with pytest.raises(ValueError):
             n.backward(t, t, None, None, Tensor((2 * 2 * shape[0],), torch.float32), t)
     assert not h._lib.calls and not n._lib.calls
+
+
+def test_maps_one_pixel_wide(monkeypatch):
+    """A column of a wider map: its pixels are a row of the map apart, whatever
+    the stride of its one column says; wider cuts are still refused."""
+    from paper_2609_16874_amd import head
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
+    h = norm()
+    t = Tensor((2, 5, 1, 8), strides=(5 * 3 * 8, 3 * 8, 8, 1))
+    assert h._map(t, "x") == (4096, 24, 120, (2, 5))
+    assert h.forward(t, None, None, t) == 0
+    assert h._map(Tensor((2, 5, 1, 8), strides=(5 * 3 * 8, 3 * 8, 1, 1)), "x")[1] == 24
+    assert h._map(Tensor((2, 1, 5, 8), strides=(99, 7, 16, 1)), "x") == (4096, 16, 99, (2, 5))
+    with pytest.raises(ValueError):
+        h._map(Tensor((2, 5, 2, 8), strides=(5 * 3 * 8, 3 * 8, 8, 1)), "x")
+
+
+@pytest.mark.gpu
+def test_one_column_of_a_wider_map():
+    from paper_2609_16874_amd import head
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn((2, 50, 3, 16), generator=g).cuda()
+    h = head.GroupNorm(2, 50, 16, 4, "f32", "silu")
+    y, stats = h.run(x[:, :, 1:2, :], None, None)
+    want, want_stats = h.run(x[:, :, 1, :].contiguous(), None, None)
+    assert torch.equal(y[:, :, 0], want) and torch.equal(stats, want_stats)
+    h.close()
