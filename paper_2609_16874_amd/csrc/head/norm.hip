@@ -26,9 +26,11 @@ namespace {
 bool strides_ok(int64_t ld, int64_t sample, int32_t samples, int32_t pixels, int32_t C)
 {
     constexpr int64_t most = (int64_t)1 << 40;
-    if (ld < C || ld > most || sample > most) return false;
+    if (ld < C || ld > most) return false;
     if (samples <= 1) return true;
-    return sample >= (int64_t)(pixels - 1) * ld + C || (sample >= C && ld >= (int64_t)(samples - 1) * sample + C);
+    if (sample < C || sample > most) return false;
+    // (by division: pixels x ld may pass 64 bits)
+    return (sample - C) / ld >= pixels - 1 || ld >= (int64_t)(samples - 1) * sample + C;
 }
 
 bool check_map(const cpe_norm *h, const void *p, int64_t ld, int64_t sample, int32_t samples, int32_t pixels)

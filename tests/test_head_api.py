@@ -151,3 +151,17 @@ def test_linear_forward_refuses_outputs_in_place_of_inputs(change):
     assert lib.cpe_linear_create(ctypes.byref(h), 4, 8, 8, 1, 0) == 0
     assert _linear_call(h, lib, y_ld=8, **change) == native.CPE_ERR_INVALID_ARG
     assert lib.cpe_linear_destroy(h) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pixels", [2 ** 23 + 1, 2 ** 24 + 1, 2 ** 31 - 2 ** 23])
+@pytest.mark.parametrize("sample", [-2 ** 62, -32, 0, 7, 2 ** 40 - 7, 2 ** 40, 2 ** 40 + 1])
+def test_norm_strides_whose_product_passes_64_bits(pixels, sample):
+    """Pixel strides of 2^40: no sample stride keeps two such samples apart."""
+    lib, h = native.library(), ctypes.c_void_p()
+    assert lib.cpe_norm_create(ctypes.byref(h), 2, 2 ** 31 - 2 ** 23, 8, 2, 1, 0, 1e-5) == 0
+    far = dict(pixels=pixels, x_ld=2 ** 40, x_sample=sample)
+    assert _norm_call(h, lib, **far) == native.CPE_ERR_INVALID_ARG
+    assert _norm_call(h, lib, pixels=pixels, x_ld=8, x_sample=8 * pixels, y_ld=2 ** 40,
+                      y_sample=sample) == native.CPE_ERR_INVALID_ARG
+    assert lib.cpe_norm_destroy(h) == 0
