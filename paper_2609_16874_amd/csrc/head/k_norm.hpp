@@ -313,7 +313,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_stats(NormArgs a)
 {
     // units of U channels of one group: a thread's vector, or a channel
     constexpr int U = GROUPED ? V : 1;
-    extern __shared__ float lds[];      // [rows][C / U] means, then M2
+    extern __shared__ __align__(16) float lds[];      // [rows][C / U] means, then M2
+    static_assert(__alignof__(lds) >= alignof(double), "the join's sums are 64-bit");
     __shared__ float counts[kNormThreads];
     const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
     const int pb = valid_pixels(a, b), C = a.channels, units = C / U;
@@ -479,7 +480,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a)
 template <typename T, int V, bool GROUPED, bool OVER, int ACT>
 __global__ __launch_bounds__(kNormThreads) void k_norm_grad_sums(NormArgs a)
 {
-    extern __shared__ float lds[];      // [rows][C] sums of du, then of du xh
+    extern __shared__ __align__(16) float lds[];      // [rows][C] sums of du, then of du xh
+    static_assert(__alignof__(lds) >= alignof(double), "the join's sums are 64-bit");
     const int b = blockIdx.x / a.blocks, i = blockIdx.x - b * a.blocks;
     const int pb = valid_pixels(a, b), C = a.channels;
     const Columns<V> cols(C);
@@ -792,7 +794,7 @@ __global__ __launch_bounds__(kGroupThreads) void k_norm_group(NormArgs a)
 template <typename T, int V, int ACT, int K>
 __global__ __launch_bounds__(kGroupThreads) void k_norm_grad_group(NormArgs a)
 {
-    extern __shared__ float lds[];      // [rows][cpg], then [lanes][cpg] and [2][cpg]
+    extern __shared__ __align__(16) float lds[];      // [rows][cpg], then [lanes][cpg] and [2][cpg]
     const GroupColumns<V> at(a);
     const int pb = valid_pixels(a, at.b), cpg = at.per_row * V, col = at.g * at.per_row + at.col;
     const T *x = static_cast<const T *>(a.x) + at.b * a.x_sample + col * V;
