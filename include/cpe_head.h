@@ -13,7 +13,8 @@
  *
  * Activations of u:  CPE_ACT_NONE u;  CPE_ACT_RELU max(u, 0) (derivative 0 at
  * 0);  CPE_ACT_SILU u / (1 + e^-u);  CPE_ACT_GELU u (1 + erf(u / sqrt 2)) / 2.
- * NaNs propagate; SiLU and GELU of -infinity are NaN (-inf * 0).
+ * NaNs propagate, through the derivatives as well; SiLU and GELU of -infinity
+ * are NaN (-inf * 0), and so are their derivatives at either infinity.
  *
  * Layouts.  Row-major; a row's elements (channels, features) are contiguous,
  * and rows are a stride apart that counts elements.  Pointers need their

@@ -70,11 +70,12 @@ __device__ __forceinline__ float activate(float u)
     return u;
 }
 
-// act'(u); ReLU's derivative at 0 is 0.
+// act'(u); ReLU's derivative at 0 is 0.  A NaN stays a NaN; SiLU's and GELU's
+// at an infinity are products inf * 0, NaNs.
 template <int ACT>
 __device__ __forceinline__ float activate_grad(float u)
 {
-    if constexpr (ACT == CPE_ACT_RELU) return u > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == CPE_ACT_RELU) return u > 0.0f ? 1.0f : u <= 0.0f ? 0.0f : u;
     if constexpr (ACT == CPE_ACT_SILU) {
         const float s = sigmoid(u);
         return s * (1.0f + u * (1.0f - s));
