@@ -43,6 +43,16 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _unrecorded(what: str, *tensors):
+    """``run`` is no node of autograd's graph: a gradient asked for through it
+    would be lost without a word."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{what} is not recorded by autograd: call it under torch.no_grad() or on detached "
+                                 "tensors, and run_backward for the gradient")
+
+
 def _int32(v, what: str) -> int:
     """A size as the C ABI's int32, which ctypes would cut off without a word."""
     v = int(v)
@@ -127,7 +137,9 @@ class GroupNorm:
             _vector(dgamma, self.channels, "dgamma", dev), _vector(dbeta, self.channels, "dbeta", dev))
 
     def run(self, x, gamma, beta, valid=None, stream=None):
-        """forward into new tensors: (y, stats)."""
+        """forward into new tensors: (y, stats).  Not recorded by autograd:
+        tensors that require a gradient are refused while it records."""
+        _unrecorded("GroupNorm.run", x, gamma, beta)
         with _allocating(stream):
             y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
             stats = torch.empty((x.shape[0], self.groups, 2), dtype=torch.float32, device=x.device)
@@ -214,7 +226,10 @@ class Linear:
                                              _vector(dbias, n, "dbias", self._device))
 
     def run(self, x, weight, bias=None, residual=None, keep=False, stream=None):
-        """forward into new tensors: y, or (y, preact) where ``keep``."""
+        """forward into new tensors: y, or (y, preact) where ``keep``.  Not
+        recorded by autograd: tensors that require a gradient are refused while
+        it records."""
+        _unrecorded("Linear.run", x, weight, bias, residual)
         with _allocating(stream):
             y = torch.empty((x.shape[0], self.out_features), dtype=x.dtype, device=x.device)
             preact = torch.empty_like(y) if keep else None

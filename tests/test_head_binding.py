@@ -236,3 +236,47 @@ def test_one_column_of_a_wider_map():
     want, want_stats = h.run(x[:, :, 1, :].contiguous(), None, None)
     assert torch.equal(y[:, :, 0], want) and torch.equal(stats, want_stats)
     h.close()
+
+
+def _needing(t):
+    t.requires_grad = True
+    return t
+
+
+@pytest.mark.parametrize("at", ["x", "gamma", "beta"])
+def test_norm_run_of_tensors_that_require_a_gradient(at, monkeypatch):
+    """An output without a gradient is not handed out where one is expected."""
+    _fake_outputs(monkeypatch)
+    h = norm()
+    a = {"x": Tensor((2, 4, 8)), "gamma": Tensor((8,), torch.float32), "beta": Tensor((8,), torch.float32)}
+    h.run(**a)
+    _needing(a[at])
+    with pytest.raises(ValueError, match="autograd"):
+        h.run(**a)
+    assert len(h._lib.calls) == 1
+    with torch.no_grad():
+        h.run(**a)
+    assert len(h._lib.calls) == 2
+
+
+@pytest.mark.parametrize("at", ["x", "weight", "bias", "residual"])
+def test_linear_run_of_tensors_that_require_a_gradient(at, monkeypatch):
+    _fake_outputs(monkeypatch)
+    h = linear()
+    a = {"x": Tensor((4, 8)), "weight": Tensor((6, 8)), "bias": Tensor((6,), torch.float32),
+         "residual": Tensor((4, 6))}
+    h.run(**a)
+    _needing(a[at])
+    with pytest.raises(ValueError, match="autograd"):
+        h.run(**a)
+    assert len(h._lib.calls) == 1
+    with torch.no_grad():
+        h.run(**a)
+    assert len(h._lib.calls) == 2
+
+
+def _fake_outputs(monkeypatch):
+    from paper_2609_16874_amd import head
+    monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
+    monkeypatch.setattr(head.torch, "empty", lambda shape, dtype=None, device=None: Tensor(
+        (shape,) if isinstance(shape, int) else shape, dtype))
