@@ -92,7 +92,8 @@ cpe_status cpe_norm_forward(cpe_norm *h, hipStream_t stream, int32_t samples, in
  *   gamma_c du and gamma_c du xh.
  * dx, dgamma, dbeta: any may be NULL (not wanted), not all.  dx may be dy or
  * x itself with the same strides.  dgamma and dbeta are written, not added to,
- * and sum over the samples; with samples or pixels 0 they are 0.
+ * and sum over the samples; with samples or pixels 0 they are 0, and all three
+ * may be NULL.
  */
 cpe_status cpe_norm_backward(cpe_norm *h, hipStream_t stream, int32_t samples, int32_t pixels, const void *x,
                              int64_t x_ld, int64_t x_sample, const void *dy, int64_t dy_ld, int64_t dy_sample,
@@ -131,7 +132,7 @@ cpe_status cpe_linear_forward(cpe_linear *h, hipStream_t stream, int32_t rows, c
  * (The residual's gradient is dy.)  preact may be NULL for CPE_ACT_NONE only.
  * dx [rows][K], dw [N][K], dbias [N] float: any may be NULL, not all; they
  * are written, not added to, and overlap no input; with rows 0, dw and dbias
- * are 0.  The products take dz rounded to the dtype, as their operand, dbias
+ * are 0, and all three may be NULL.  The products take dz rounded to the dtype, as their operand, dbias
  * sums it unrounded.
  */
 cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, const void *x, int64_t x_ld,

@@ -152,7 +152,7 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
 {
     const cpe_status st = check_call(h, rows);
     if (st != CPE_OK) return st;
-    if (!dx && !dw && !dbias) return CPE_ERR_INVALID_ARG;
+    if (rows > 0 && !dx && !dw && !dbias) return CPE_ERR_INVALID_ARG;      // (a dx of no rows has no pointer)
     if (!aligned_to(dbias, 4)) return CPE_ERR_INVALID_ARG;
     const bool act = h->act != CPE_ACT_NONE;
     if (rows > 0) {

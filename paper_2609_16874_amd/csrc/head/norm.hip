@@ -164,7 +164,8 @@ cpe_status cpe_norm_backward(cpe_norm *h, hipStream_t stream, int32_t samples, i
 {
     const cpe_status st = check_call(h, samples, pixels, gamma, beta, valid);
     if (st != CPE_OK) return st;
-    if (!dx && !dgamma && !dbeta) return CPE_ERR_INVALID_ARG;
+    // (a dx of nothing has no pointer)
+    if (samples > 0 && pixels > 0 && !dx && !dgamma && !dbeta) return CPE_ERR_INVALID_ARG;
     if (!aligned_to(dgamma, 4) || !aligned_to(dbeta, 4) || !aligned_to(stats, 8)) return CPE_ERR_INVALID_ARG;
     NormArgs a = common_args(h, samples, pixels, gamma, beta, valid);
     a.backward = true;

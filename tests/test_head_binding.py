@@ -280,3 +280,19 @@ def _fake_outputs(monkeypatch):
     monkeypatch.setattr(head, "_stream", lambda stream, device: 0)
     monkeypatch.setattr(head.torch, "empty", lambda shape, dtype=None, device=None: Tensor(
         (shape,) if isinstance(shape, int) else shape, dtype))
+
+
+@pytest.mark.gpu
+def test_gradient_of_nothing_asked_for_dx_alone():
+    """An empty dx has no pointer: it is not taken for one that is not wanted."""
+    from paper_2609_16874_amd import head
+    h = head.Linear(4, 8, 6, "f16", "silu")
+    x, e, w = (torch.empty(s, dtype=torch.float16, device="cuda") for s in ((0, 8), (0, 6), (6, 8)))
+    assert h.backward(x, w, e, e, dx=torch.empty_like(x)) == 0
+    h.close()
+    n = head.GroupNorm(2, 4, 8, 2, "f16", "silu")
+    for shape in ((0, 4, 8), (2, 0, 8)):
+        x = torch.empty(shape, dtype=torch.float16, device="cuda")
+        stats = torch.zeros((shape[0], 2, 2), device="cuda")
+        assert n.backward(x, x, None, None, stats, dx=torch.empty_like(x)) == 0
+    n.close()
