@@ -78,11 +78,11 @@ class GroupNorm:
     def __init__(self, max_samples: int, max_pixels: int, channels: int, groups: int, dtype: str,
                  activation: str = "none", eps: float = 1e-5):
         self.channels, self.groups, self.dtype = _int32(channels, "channels"), _int32(groups, "groups"), dtype
-        self._torch_dtype, self._lib = torch_dtype(dtype), library()
+        self.eps, self._torch_dtype, self._lib = float(eps), torch_dtype(dtype), library()
         h = ctypes.c_void_p()
         st = self._lib.cpe_norm_create(ctypes.byref(h), _int32(max_samples, "max_samples"),
                                        _int32(max_pixels, "max_pixels"), self.channels, self.groups,
-                                       DTYPES[dtype], ACTIVATIONS[activation], float(eps))
+                                       DTYPES[dtype], ACTIVATIONS[activation], self.eps)
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_create")
         self._h, self._device = h, torch.cuda.current_device()
@@ -143,6 +143,9 @@ class GroupNorm:
         with _allocating(stream):
             y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
             stats = torch.empty((x.shape[0], self.groups, 2), dtype=torch.float32, device=x.device)
+            if x.numel() == 0:      # the call has nothing to do: what it says of samples without pixels
+                stats[..., 0] = 0.0
+                stats[..., 1] = self.eps ** -0.5
         st = self.forward(x, gamma, beta, y, stats, valid, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_norm_forward")

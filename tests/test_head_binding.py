@@ -296,3 +296,16 @@ def test_gradient_of_nothing_asked_for_dx_alone():
         stats = torch.zeros((shape[0], 2, 2), device="cuda")
         assert n.backward(x, x, None, None, stats, dx=torch.empty_like(x)) == 0
     n.close()
+
+
+@pytest.mark.gpu
+def test_run_of_maps_without_pixels_gives_their_statistics():
+    from paper_2609_16874_amd import head
+    n = head.GroupNorm(2, 4, 8, 2, "f16", "silu", 0.25)
+    for _ in range(3):
+        scrap = torch.full((2, 2, 2), 77.0, device="cuda")       # what new memory may hold
+        del scrap
+        y, stats = n.run(torch.empty((2, 0, 8), dtype=torch.float16, device="cuda"), None, None)
+        assert y.shape == (2, 0, 8)
+        assert stats.tolist() == [[[0.0, 2.0]] * 2] * 2
+    n.close()
