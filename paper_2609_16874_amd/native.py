@@ -7,6 +7,7 @@ the library has not been built this module raises; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -275,7 +276,12 @@ class Decoder:
         """Decode one frame, synchronise, and return host numpy results
         (cpe_decode_ex when ``tau`` is given or ``fg`` is None)."""
         import torch
-        out = outputs or self.new_outputs(emb.device, score)
+        out = outputs
+        if not out:
+            # on the stream that writes them: theirs may be a block that the
+            # current stream still uses, and two of them are zeroed there first
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+                out = self.new_outputs(emb.device, score)
         if tau is None and fg is not None:
             st = self.decode(emb, fg, fg_threshold, peak_threshold, out["centroids"], out["num_centroids"],
                              out["labels"], out["score_map"], stream)
