@@ -109,6 +109,11 @@ size_t cpe_norm_workspace_bytes(const cpe_norm *h);
  * Matrix product with an epilogue: z = x w^T + bias, y = act(z) + residual.
  *   max_rows       1..2^31 - 2^23 rows (pixels, tokens) of a call at most
  *   in_features    K, 1..65536; out_features N, 1..65536
+ * The handle's scratch is what calls of up to max_rows rows can use: up to
+ * 32 MiB for products split along k and their gradients' partial sums, up to 8
+ * MiB for those of dbias, and, with an activation, max_rows x N of the dtype for
+ * dz where the gradient is neither one of few rows (up to 64) nor, in 16 bits,
+ * narrow (N and K multiples of 8, up to 128 x 256 or 64 x 512).
  */
 cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_features, int32_t out_features,
                              cpe_head_dtype dtype, cpe_activation act);

@@ -37,7 +37,7 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 template <typename T>
 constexpr int kChunk = 16 / (int)sizeof(T);           // elements in 16 bytes
 template <typename T>
-constexpr int kStepK = 8 * kChunk<T>;                 // k of one LDS tile
+constexpr int kStepK = step_k(sizeof(T));
 
 union Fragment {
     u32x4 u;
@@ -635,7 +635,7 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
         const int n = (first + col) * V;
         const T *pd = static_cast<const T *>(g.dy) + n, *pz = static_cast<const T *>(g.preact) + n;
         T *po = static_cast<T *>(g.dz) + n;
-        constexpr int U = 4;
+        constexpr int U = kSumUnroll;
         for (int64_t r = lo + row; r < hi; r += U * rows) {
             Vec<T, V> d[U], z[U];
 #pragma unroll
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(1024) void k_column_join(GradArgs g)
 // LDS rows of 16-byte chunks, chunk c of row r at c ^ f(r) (rows of 128 bytes)
 // or c ^ 2 f(r): f differs over eight rows in a row and over the rows r .. r+3,
 // r+8 .. r+11 that half a transposing read's lanes name.
-constexpr int kStripRows = 64, kNarrowThreads = 512;
+constexpr int kNarrowThreads = 512;
 __device__ __forceinline__ int strip_swizzle(int row, int chunks)
 {
     const int f = (row & 3) | (((row >> 3) ^ (row >> 2)) & 1) << 2;
@@ -1034,7 +1034,7 @@ bool direct_ok(const GemmArgs &g)
 template <typename T>
 void choose_splits(GemmArgs &g)
 {
-    constexpr int kLeast = sizeof(T) == 4 ? 4 : 8;
+    constexpr int kLeast = least_steps(sizeof(T));
     const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n, steps = g.k > 0 ? ceil_div(g.k, kStepK<T>) : 1;
     int64_t splits = kSplitTiles / tiles;
     if (splits > 1 && steps / splits < 2 * kLeast) {
@@ -1042,7 +1042,7 @@ void choose_splits(GemmArgs &g)
         if (splits > steps / kLeast) splits = steps / kLeast;
     }
     const int64_t one = (int64_t)g.m * ceil_div(g.n, 4) * 16;      // a split's partial outputs, in the scratch
-    if (splits > kSplitBytes / one) splits = kSplitBytes / one;
+    if (splits > g.part_bytes / one) splits = g.part_bytes / one;
     if (splits < 1) splits = 1;
     const int64_t each = ceil_div(steps, splits);
     g.k_split = (int32_t)(each * kStepK<T>);
@@ -1182,7 +1182,7 @@ hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
         g.slab = 256;
         rows = vectors >= 256 ? 1 : 256 / vectors;
         const int64_t slabs = ceil_div(vectors, 256);
-        const int64_t want = ceil_div(g.rows, 4 * (int64_t)rows), cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
+        const int64_t want = ceil_div(g.rows, kSumUnroll * (int64_t)rows), cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
         g.blocks = (int32_t)(want < 1 ? 1 : want < cap ? want : cap);
     }
     const int64_t slabs = ceil_div(vectors, g.slab);
@@ -1258,7 +1258,7 @@ hipError_t launch_narrow_grad_type(WholeGradArgs a, hipStream_t stream)
 {
     // one workgroup per CU: a second one would double the partial dw
     const int64_t strips = ceil_div(a.rows, kStripRows);
-    a.blocks = (int32_t)(strips < 256 ? strips : 256);
+    a.blocks = (int32_t)(strips < kNarrowGradBlocks ? strips : kNarrowGradBlocks);
     const bool wide_n = a.n > 64;
     hipError_t e;
     if (a.k <= 128)

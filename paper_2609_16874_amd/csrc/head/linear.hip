@@ -14,7 +14,7 @@ struct cpe_linear {
     cpe_activation act;
     int device;
     unsigned char *ws;
-    size_t ws_bytes, sums_at, dz_at;
+    size_t ws_bytes, split_bytes, sums_at, dz_at;
     int64_t dz_ld;
 };
 
@@ -50,10 +50,10 @@ hipError_t launch_grad(const cpe_linear *h, const GradArgs &g, hipStream_t strea
 // The gradient in one pass: whole vectors of features and a dw that eight
 // waves' registers hold.  14.5 us against 24 .. 36 for the three products from
 // 100 to 4000 rows (64 to 256 features), 110 against 200 at 409,600.
-bool narrow_grad_fits(const WholeGradArgs &a)
+bool narrow_grad_fits(int32_t rows, int32_t n, int32_t k, cpe_head_dtype dtype)
 {
-    if (a.rows < 1 || a.n % 8 != 0 || a.k % 8 != 0) return false;
-    return (a.n <= 128 && a.k <= 256) || (a.n <= 64 && a.k <= 512);
+    if (dtype == CPE_HEAD_F32 || rows < 1 || n % 8 != 0 || k % 8 != 0) return false;
+    return (n <= 128 && k <= 256) || (n <= 64 && k <= 512);
 }
 
 // Few rows: two launches instead of four or five, 14 us against 20 on small
@@ -62,10 +62,49 @@ bool narrow_grad_fits(const WholeGradArgs &a)
 // ones: bf16 16 x 2048 to 4096 46 us against 33, 64 x 1024 to 1024 29 against
 // 27; binary32, whose tiles waste more on rows that are not there, 23 x 3776 to
 // 1152 28 against 39.
-bool rows_grad_fits(const WholeGradArgs &a, cpe_head_dtype dtype)
+bool rows_grad_fits(int32_t rows, int32_t n, int32_t k, cpe_head_dtype dtype)
 {
     const int64_t most = (int64_t)1 << (dtype == CPE_HEAD_F32 ? 27 : 25);
-    return a.rows >= 1 && a.rows <= 64 && (int64_t)a.rows * a.n * a.k <= most;
+    return rows >= 1 && rows <= 64 && (int64_t)rows * n * k <= most;
+}
+
+// The most that the splits of a product of up to m x n outputs over up to k can
+// fill: each split has least_steps or more, and all of them kSplitBytes or less.
+int64_t most_split_bytes(size_t element, int64_t m, int64_t n, int64_t k)
+{
+    const int64_t splits = ceil_div(k, step_k(element)) / least_steps(element);
+    if (splits < 2) return 0;
+    const int64_t bytes = splits * m * ceil_div(n, 4) * 16;
+    return bytes < kSplitBytes ? bytes : kSplitBytes;
+}
+
+// The handle's scratch: what some call of up to max_rows rows fills.
+void plan_scratch(cpe_linear *h)
+{
+    const int64_t rows = h->max_rows, n = h->out, k = h->in;
+    const size_t size = element_size(h->dtype);
+    int64_t split = most_split_bytes(size, rows, n, k), sums = 0, dz = 0;
+    // (a gradient that fits the few-row kernels at max_rows does at fewer, and needs none)
+    if (!rows_grad_fits(h->max_rows, h->out, h->in, h->dtype)) {
+        // partial sums of dbias: at most kSumBlocks workgroups, kSumUnroll rows or more
+        // in each, and fewer workgroups above 2048 columns (kSumBlocks / slabs)
+        const int64_t dealt = ceil_div(rows, kSumUnroll) * n, most = (int64_t)kSumBlocks * (n < 2048 ? n : 2048);
+        sums = (dealt < most ? dealt : most) * 4;
+        int64_t part;
+        if (narrow_grad_fits(1, h->out, h->in, h->dtype)) {
+            const int64_t strips = ceil_div(rows, kStripRows);
+            part = (strips < kNarrowGradBlocks ? strips : kNarrowGradBlocks) * n * k * 4;
+        } else {
+            const int64_t dx = most_split_bytes(size, rows, k, n), dw = most_split_bytes(size, n, k, rows);
+            part = dx > dw ? dx : dw;
+            if (h->act != CPE_ACT_NONE) dz = rows * h->dz_ld * (int64_t)size;
+        }
+        if (part > split) split = part;
+    }
+    h->split_bytes = (size_t)split;
+    h->sums_at = align256(h->split_bytes);
+    h->dz_at = h->sums_at + align256((size_t)sums);
+    h->ws_bytes = h->dz_at + align256((size_t)dz);
 }
 
 }  // namespace
@@ -94,12 +133,9 @@ cpe_status cpe_linear_create(cpe_linear **out, int32_t max_rows, int32_t in_feat
         return CPE_ERR_HIP;
     }
     h->dz_ld = (out_features + 7) / 8 * 8;
-    h->sums_at = align256((size_t)kSplitBytes);
-    h->dz_at = h->sums_at + align256((size_t)kSumBlocks * (out_features < 2048 ? out_features : 2048) * 4);
-    h->ws_bytes = h->dz_at;
-    if (act != CPE_ACT_NONE) h->ws_bytes += align256((size_t)max_rows * h->dz_ld * element_size(dtype));
+    plan_scratch(h);
     void *p = nullptr;
-    if (hipMalloc(&p, h->ws_bytes) != hipSuccess) {
+    if (h->ws_bytes > 0 && hipMalloc(&p, h->ws_bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete h;
         return CPE_ERR_OUT_OF_MEMORY;
@@ -142,6 +178,7 @@ cpe_status cpe_linear_forward(cpe_linear *h, hipStream_t stream, int32_t rows, c
     g.ldp = preact_ld;
     g.act = h->act;
     g.part = reinterpret_cast<float *>(h->ws);
+    g.part_bytes = (int64_t)h->split_bytes;
     (void)hipGetLastError();
     return launch_gemm(h, g, stream) == hipSuccess ? CPE_OK : CPE_ERR_HIP;
 }
@@ -187,13 +224,13 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
         a.n = h->out;
         a.k = h->in;
         a.act = h->act;
-        if (rows_grad_fits(a, h->dtype)) {
+        if (rows_grad_fits(rows, h->out, h->in, h->dtype)) {
             const hipError_t e = h->dtype == CPE_HEAD_F32   ? launch_rows_grad_f32(a, stream)
                                  : h->dtype == CPE_HEAD_F16 ? launch_rows_grad_f16(a, stream)
                                                        : launch_rows_grad_bf16(a, stream);
             return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
         }
-        if (h->dtype != CPE_HEAD_F32 && narrow_grad_fits(a)) {
+        if (narrow_grad_fits(rows, h->out, h->in, h->dtype)) {
             const hipError_t e = h->dtype == CPE_HEAD_F16 ? launch_narrow_grad_f16(a, stream)
                                                      : launch_narrow_grad_bf16(a, stream);
             return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
@@ -233,6 +270,7 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
         g.out = dx;
         g.ldo = dx_ld;
         g.part = reinterpret_cast<float *>(h->ws);
+        g.part_bytes = (int64_t)h->split_bytes;
         if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
     }
     if (dw) {                   // dw[n][k] = sum_r dz[r][n] x[r][k]
@@ -249,6 +287,7 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
         g.out = dw;
         g.ldo = dw_ld;
         g.part = reinterpret_cast<float *>(h->ws);
+        g.part_bytes = (int64_t)h->split_bytes;
         if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
     }
     return CPE_OK;

@@ -13,8 +13,13 @@ constexpr int kGemmThreads = 256;
 constexpr int kTile = 128;                    // output rows and columns of a workgroup
 constexpr int kSplitTiles = 512;              // partial tiles of a split product
 constexpr int64_t kSplitBytes = (int64_t)kSplitTiles * kTile * kTile * 4;       // and their scratch
+constexpr int step_k(size_t element) { return 128 / (int)element; }             // k of one LDS tile
+constexpr int least_steps(size_t element) { return element == 4 ? 4 : 8; }      // of a split
 constexpr int64_t kMaxTiles = (int64_t)1 << 22;
 constexpr int kSumBlocks = 1024;              // workgroups along the rows of the bias gradient
+constexpr int kStripRows = 64;                // rows that a workgroup of the one-pass gradient takes at a time
+constexpr int kNarrowGradBlocks = 256;        // and its workgroups
+constexpr int kSumUnroll = 4;                 // rows of a thread of the bias gradient in flight
 
 // out[m][n] = act(sum_k A(m, k) B(n, k) + bias[n]) + residual[m][n].
 // A(m, k) is a[m lda + k], or a[k lda + m] where a_cols is set; B alike.
@@ -32,6 +37,7 @@ struct GemmArgs {
     int64_t ldp;
     int act;
     float *part;                              // scratch of a split product: [splits][m][n rounded up to 4]
+    int64_t part_bytes;
     int32_t splits, k_split;                  // splits > 1: each sums k_split of the k
     int32_t tiles_m, tiles_n;
 };
