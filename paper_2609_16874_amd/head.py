@@ -64,7 +64,7 @@ def _vector(t, n: int, name: str, device: int, dtype=torch.float32):
     """The pointer of a contiguous device vector, or None."""
     if t is None:
         return None
-    if not (t.is_cuda and t.get_device() == device and t.dtype is dtype and t.numel() == n and t.is_contiguous()):
+    if not (t.get_device() == device and t.dtype is dtype and t.numel() == n and t.is_contiguous()):
         raise ValueError(f"{name}: a contiguous tensor of {n} {dtype} on the handle's device is needed")
     return t.data_ptr()
 
@@ -74,6 +74,7 @@ class GroupNorm:
     calls of up to ``max_samples`` samples of ``max_pixels`` pixels.  Maps are
     [samples][pixels][C] tensors (or [samples][H][W][C] ones whose rows follow
     one another) with contiguous channels; other strides are free."""
+    _device = None      # the handle's; a host tensor's get_device() is -1
 
     def __init__(self, max_samples: int, max_pixels: int, channels: int, groups: int, dtype: str,
                  activation: str = "none", eps: float = 1e-5):
@@ -101,14 +102,13 @@ class GroupNorm:
             _need(height <= 1 or width <= 1 or strides[1] == width * strides[2],
                   f"{name}: image rows must follow one another")
             ld = strides[2] if width > 1 else strides[1]
-        if not (t.is_cuda and t.get_device() == self._device and t.dtype is self._torch_dtype
-                and channels == self.channels and (channels == 1 or strides[-1] == 1)
-                and (size is None or size == (samples, pixels))):
+        if not (t.get_device() == self._device and t.dtype is self._torch_dtype and channels == self.channels
+                and (channels == 1 or strides[-1] == 1) and (size is None or size == (samples, pixels))):
             raise ValueError(f"{name}: wrong shape, dtype, device or channel stride")
         if pixels <= 1 and ld < channels:      # the stride of a single pixel says nothing
             ld = channels
-        if size is None:
-            samples, pixels = _int32(samples, name), _int32(pixels, name)
+        if size is None and (samples >> 31 or pixels >> 31):
+            raise ValueError(f"{name}: {samples} x {pixels} are no 32-bit sizes")
         return t.data_ptr(), ld, strides[0], (samples, pixels)
 
     def forward(self, x, gamma, beta, y, stats=None, valid=None, stream=None) -> int:
@@ -180,6 +180,7 @@ class Linear:
     """Handle of one matrix product (features, dtype, activation) for calls of
     up to ``max_rows`` rows.  Matrices are [rows][features] tensors with
     contiguous features and any row stride; the weight is [out][in]."""
+    _device = None      # the handle's; a host tensor's get_device() is -1
 
     def __init__(self, max_rows: int, in_features: int, out_features: int, dtype: str, activation: str = "none"):
         self.in_features, self.out_features = _int32(in_features, "in_features"), _int32(out_features, "out_features")
@@ -197,7 +198,7 @@ class Linear:
         if t is None:
             return None, 0
         shape, strides = t.shape, t.stride()
-        if not (len(shape) == 2 and t.is_cuda and t.get_device() == self._device and t.dtype is self._torch_dtype
+        if not (len(shape) == 2 and t.get_device() == self._device and t.dtype is self._torch_dtype
                 and shape[1] == width and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
             raise ValueError(f"{name}: wrong shape, dtype, device or feature stride")
         ld = strides[0]
@@ -206,7 +207,9 @@ class Linear:
     def forward(self, x, weight, bias, y, residual=None, preact=None, stream=None) -> int:
         """cpe_linear_forward: ``preact`` receives the value before the
         activation, which the gradient needs."""
-        rows, n = _int32(x.shape[0], "rows"), self.out_features
+        rows, n = x.shape[0], self.out_features
+        if rows >> 31:
+            raise ValueError(f"x: {rows} is no 32-bit number of rows")
         px, x_ld = self._matrix(x, None, self.in_features, "x")
         pw, w_ld = self._matrix(weight, n, self.in_features, "weight")
         py, y_ld = self._matrix(y, rows, n, "y")
@@ -217,7 +220,9 @@ class Linear:
 
     def backward(self, x, weight, dy, preact=None, dx=None, dweight=None, dbias=None, stream=None) -> int:
         """cpe_linear_backward: writes those of dx, dweight and dbias that are given."""
-        rows, k, n = _int32(x.shape[0], "rows"), self.in_features, self.out_features
+        rows, k, n = x.shape[0], self.in_features, self.out_features
+        if rows >> 31:
+            raise ValueError(f"x: {rows} is no 32-bit number of rows")
         px, x_ld = self._matrix(x, None, k, "x")
         pw, w_ld = self._matrix(weight, n, k, "weight")
         pd, d_ld = self._matrix(dy, rows, n, "dy")
