@@ -137,8 +137,9 @@ cpe_status cpe_linear_forward(cpe_linear *h, hipStream_t stream, int32_t rows, c
  * (The residual's gradient is dy.)  preact may be NULL for CPE_ACT_NONE only.
  * dx [rows][K], dw [N][K], dbias [N] float: any may be NULL, not all; they
  * are written, not added to, and overlap no input; with rows 0, dw and dbias
- * are 0, and all three may be NULL.  The products take dz rounded to the dtype, as their operand, dbias
- * sums it unrounded.
+ * are 0, and all three may be NULL.  The products take dz rounded to the dtype,
+ * as their operand (in f16 a |dz| beyond 65504, which takes a |dy| beyond 57,000,
+ * becomes an infinity); dbias sums it unrounded.
  */
 cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, const void *x, int64_t x_ld,
                                const void *w, int64_t w_ld, const void *dy, int64_t dy_ld, const void *preact,

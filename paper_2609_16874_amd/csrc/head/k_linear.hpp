@@ -13,6 +13,14 @@
 // B fragment goes first, so that a lane's four accumulators are neighbouring
 // n of one row m and are stored as one vector.
 //
+// The gradient's products take dz = dy act'(z) as an operand of these
+// instructions, so it is rounded to the type first (in 32 bits it stays as it
+// is).  To keep more of it would take a second operand for its low half and
+// twice the products, which are 145 of the 198 us of a large gradient.  The
+// rounding is as large as the outputs' own: dx and dw are off by 2.9e-4 instead
+// of 2.1e-4 in f16 and 2.3e-3 instead of 1.7e-3 in bf16 (2-norm of the error
+// over that of the result; 409,600 x 256 to 64 and 7744 x 1024 to 4096).
+//
 // LDS tiles hold 128 bytes of k.  Along k: a row per m (or n) of eight
 // 16-byte chunks, chunk c of row r at place c ^ (r & 7).  Across k: a row per
 // k, read back through the transposing LDS read (16 bits), its 32-byte units
