@@ -1190,7 +1190,8 @@ hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
         g.slab = 256;
         rows = vectors >= 256 ? 1 : 256 / vectors;
         const int64_t slabs = ceil_div(vectors, 256);
-        const int64_t want = ceil_div(g.rows, kSumUnroll * (int64_t)rows), cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
+        const int64_t want = ceil_div(g.rows, kSumUnroll * (int64_t)rows);
+        const int64_t cap = kSumBlocks / slabs < 1 ? 1 : kSumBlocks / slabs;
         g.blocks = (int32_t)(want < 1 ? 1 : want < cap ? want : cap);
     }
     const int64_t slabs = ceil_div(vectors, g.slab);

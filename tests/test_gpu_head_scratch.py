@@ -35,8 +35,8 @@ def test_handles_hold_what_their_calls_can_use():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("M,K,N", [(1, 1024, 1024), (65, 2048, 136), (200, 1024, 1024), (400, 700, 760), (400, 520, 4104),
-                                   (1500, 1024, 64), (700, 64, 48), (64, 1000, 264), (130, 4096, 72)])
+@pytest.mark.parametrize("M,K,N", [(1, 1024, 1024), (65, 2048, 136), (200, 1024, 1024), (400, 700, 760),
+                                   (400, 520, 4104), (1500, 1024, 64), (700, 64, 48), (64, 1000, 264), (130, 4096, 72)])
 def test_the_size_of_a_handle_changes_no_result(M, K, N, dtype):
     """A handle for M rows and one for many more."""
     print(f"scratch of {M} {K} {N} {dtype}", flush=True)
