@@ -1,9 +1,10 @@
 """Compile the gfx950 HIP library ``libcpe_decode.so`` in-tree with hipcc.
 
 The kernel instantiations are split over several translation units
-(``csrc/launch_*.hip``, ``csrc/head/*_*.hip``) that are compiled in parallel,
-then linked with the host parts (``csrc/cpe_decode.hip``, ``csrc/head/norm.hip``,
-``csrc/head/linear.hip``) into one shared library.
+(``csrc/launch_*.hip``, ``csrc/head/*_*.hip``, ``csrc/rows8/*_*.hip``) that are
+compiled in parallel, then linked with the host parts (``csrc/cpe_decode.hip``,
+``csrc/head/norm.hip``, ``csrc/head/linear.hip``, ``csrc/rows8/rows8.hip``,
+``csrc/rows8/linear8.hip``) into one shared library.
 """
 from __future__ import annotations
 
@@ -28,7 +29,7 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "head", "*.hip")))
+    return sorted(p for folder in ("", "head", "rows8") for p in glob.glob(os.path.join(CSRC, folder, "*.hip")))
 
 
 def build(verbose: bool = False, jobs: int = 8) -> str:

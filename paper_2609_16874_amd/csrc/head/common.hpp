@@ -87,6 +87,19 @@ __device__ __forceinline__ float activate_grad(float u)
     return 1.0f;
 }
 
+// A binary32 result that is rounded to T as it stands.  (In f16 the compiler
+// makes one instruction of a product or sum and its conversion, which rounds
+// once, but not everywhere: equal operands would give different values.)
+template <typename T>
+__device__ __forceinline__ T rounded(float x)
+{
+    if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(x));
+    return (T)x;
+}
+// A byte times its row's scale.
+template <typename T>
+__device__ __forceinline__ T scaled_byte(int8_t q, float scale) { return rounded<T>((float)q * scale); }
+
 // The work that workgroup w of n takes: workgroups are dealt to the eight XCDs
 // in turn, so this gives each XCD a run of neighbours, which share lines of
 // its L2.

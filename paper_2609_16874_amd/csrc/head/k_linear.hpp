@@ -90,6 +90,21 @@ __device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left)
     return f.u;
 }
 
+// A row's scale as f p: where FOLD, f is its mantissa (1 <= f < 2) and p a
+// power of two, by which bytes are exact in 16 bits; otherwise f is 1.  (So it
+// is for scales without a mantissa: 0, infinities, NaNs, subnormal ones.)
+struct ScaleParts {
+    float f, p;
+};
+template <bool FOLD>
+__device__ __forceinline__ ScaleParts scale_parts(float s)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, s);
+    const bool normal = FOLD && ((b >> 23) & 255) - 1 < 254;
+    return {normal ? __builtin_bit_cast(float, (b & 0x007fffffu) | 0x3f800000u) : 1.0f,
+            normal ? __builtin_bit_cast(float, b & 0xff800000u) : s};
+}
+
 // One operand of a workgroup: R rows (m or n) by kStepK of k.  DIRECT: loads
 // through a buffer descriptor straight into LDS; a lane out of range has an
 // offset beyond the descriptor's, which reads as 0.
@@ -201,6 +216,66 @@ struct Operand {
     }
 };
 
+// An operand across k of which each k is a row in 8 bits: bytes come into
+// registers, and become elements on their way to LDS, where they lie as
+// those of Operand<T, true>.
+template <typename T>
+struct PackedOperand : Operand<T, true, false> {
+    using O = Operand<T, true, false>;
+    static constexpr int E = O::E, kLoads = O::kLoads;
+    const int8_t *from[kLoads];
+    const float *scales;
+    int64_t step8;
+    int columns[kLoads];
+    Vec<int8_t, E> bytes[kLoads];
+    float scale[kLoads];
+    bool fold;
+
+    __device__ __forceinline__ void init(const GemmArgs &g, int r0, int k0)
+    {
+        step8 = kStepK<T> * g.ldb;
+        scales = g.b_scale + k0;
+        fold = g.fold;
+        const int8_t *first = static_cast<const int8_t *>(g.b) + k0 * g.ldb + r0;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int row = O::row_of(i), c = O::chunk_of(i);
+            columns[i] = g.n - r0 - c * E;
+            from[i] = first + row * g.ldb + c * E;
+        }
+    }
+    template <bool TAIL>
+    __device__ __forceinline__ void fetch(lds_byte *, int left)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const bool there = !TAIL || O::row_of(i) < left;
+            scale[i] = there ? scales[O::row_of(i)] : 0.0f;
+            if (there && columns[i] >= E) {
+                bytes[i] = load_vec<int8_t, E>(from[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; e++) bytes[i].v[e] = there && e < columns[i] ? from[i][e] : (int8_t)0;
+            }
+            from[i] += step8;
+        }
+        scales += kStepK<T>;
+    }
+    __device__ __forceinline__ void commit(lds_byte *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const float p = fold ? scale_parts<true>(scale[i]).p : scale[i];
+            T e[E];
+#pragma unroll
+            for (int v = 0; v < E; v++) e[v] = scaled_byte<T>(bytes[i].v[v], p);
+            Fragment f;
+            __builtin_memcpy(&f, e, 16);
+            *(__attribute__((address_space(3))) u32x4 *)(lds + (i * kGemmThreads + threadIdx.x) * 16) = f.u;
+        }
+    }
+};
+
 // W neighbouring outputs of row m: bias, the value kept for the gradient,
 // activation, residual, each rounded once.
 template <int ACT, typename T, int W>
@@ -210,6 +285,13 @@ __device__ __forceinline__ void finish(const GemmArgs &g, int m, int n, float (&
     T *out = static_cast<T *>(g.out) + m * g.ldo + n;
     const T *res = g.residual ? static_cast<const T *>(g.residual) + m * g.ldr + n : nullptr;
     T *pre = g.preact ? static_cast<T *>(g.preact) + m * g.ldp + n : nullptr;
+    if constexpr (ACT == CPE_ACT_NONE && sizeof(T) == 2) {
+        if (g.row_scale) {
+            const float f = 1.0f / scale_parts<true>(g.row_scale[m]).f;
+#pragma unroll
+            for (int i = 0; i < W; i++) v[i] *= f;
+        }
+    }
     if (left >= W) {
         Vec<T, W> o;
         if (g.bias) {
@@ -283,11 +365,11 @@ __device__ __forceinline__ void meet()
 // (0.14).  A smaller share of LDS reads (larger tiles) gains only where no split
 // is needed; deeper staging and 32 x 32 instructions gain nothing.
 constexpr int kBand = 8;
-template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT>
+template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT, bool PACKED = false>
 __global__ __launch_bounds__(kGemmThreads, 2) void k_gemm(GemmArgs g)
 {
     using A = Operand<T, A_ACROSS, DIRECT>;
-    using B = Operand<T, B_ACROSS, DIRECT>;
+    using B = std::conditional_t<PACKED, PackedOperand<T>, Operand<T, B_ACROSS, DIRECT>>;
     constexpr int kStage = A::kBytes + B::kBytes, W = kTile / 32;       // fragments of a wave's rows
     __shared__ __align__(1024) unsigned char smem[2 * kStage];
     static_assert(2 * kStage >= kTile * kTile * 4, "the epilogue's tile fits");
@@ -308,7 +390,10 @@ __global__ __launch_bounds__(kGemmThreads, 2) void k_gemm(GemmArgs g)
     A a;
     B b;
     a.init(g.a, g.lda, m0, g.m, k0);
-    b.init(g.b, g.ldb, n0, g.n, k0);
+    if constexpr (PACKED)
+        b.init(g, n0, k0);
+    else
+        b.init(g.b, g.ldb, n0, g.n, k0);
     f32x4 acc[W][W];
 #pragma unroll
     for (int i = 0; i < W; i++)
@@ -628,9 +713,12 @@ __global__ __launch_bounds__(256, 2) void k_gemm_narrow(GemmArgs g)
 // over this workgroup's rows, unrounded.  Bound by memory and, for GELU, the
 // vector unit (61 % busy): 46 us for 7744 x 4096 in bf16 (4.1 TB/s).  A workgroup
 // covers g.slab vectors of V columns (blockIdx.y) and 256 / vectors rows at a time.
-template <typename T, int V, int ACT>
+// PACKED: preact is rows in 8 bits, and dz is multiplied by the mantissa of its
+// row's scale of x where the products take it so.
+template <typename T, int V, int ACT, bool PACKED>
 __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
 {
+    using Z = std::conditional_t<PACKED, int8_t, T>;
     __shared__ float lds[256 * V];
     const int all = g.n / V, first = blockIdx.y * g.slab, here = all - first < g.slab ? all - first : g.slab;
     const int rows = 256 / here, row = threadIdx.x / here, col = threadIdx.x - row * here;
@@ -641,17 +729,24 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
     for (int v = 0; v < V; v++) sum[v] = 0.0f;
     if (row < rows) {
         const int n = (first + col) * V;
-        const T *pd = static_cast<const T *>(g.dy) + n, *pz = static_cast<const T *>(g.preact) + n;
+        const T *pd = static_cast<const T *>(g.dy) + n;
+        const Z *pz = static_cast<const Z *>(g.preact) + n;
         T *po = static_cast<T *>(g.dz) + n;
         constexpr int U = kSumUnroll;
         for (int64_t r = lo + row; r < hi; r += U * rows) {
-            Vec<T, V> d[U], z[U];
+            Vec<T, V> d[U];
+            Vec<Z, V> z[U];
+            [[maybe_unused]] float z_scale[U], x_scale[U];
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 const int64_t at = r + u * rows;
                 if (at < hi) {
                     d[u] = load_vec<T, V>(pd + at * g.ldd);
-                    if (ACT != CPE_ACT_NONE) z[u] = load_vec<T, V>(pz + at * g.ldp);
+                    if (ACT != CPE_ACT_NONE) z[u] = load_vec<Z, V>(pz + at * g.ldp);
+                    if constexpr (PACKED) {
+                        z_scale[u] = g.z_scale[at];
+                        x_scale[u] = folds(ACT, sizeof(T)) ? g.x_scale[at] : 1.0f;
+                    }
                 }
             }
 #pragma unroll
@@ -659,11 +754,14 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
                 const int64_t at = r + u * rows;
                 if (at >= hi) continue;
                 Vec<T, V> o;
+                [[maybe_unused]] const float f = PACKED ? scale_parts<true>(x_scale[u]).f : 1.0f;
 #pragma unroll
                 for (int v = 0; v < V; v++) {
                     float dz = (float)d[u].v[v];
-                    if constexpr (ACT != CPE_ACT_NONE) dz *= activate_grad<ACT>((float)z[u].v[v]);
+                    if constexpr (ACT != CPE_ACT_NONE)
+                        dz *= activate_grad<ACT>(PACKED ? (float)z[u].v[v] * z_scale[u] : (float)z[u].v[v]);
                     sum[v] += dz;
+                    if constexpr (PACKED && folds(ACT, sizeof(T))) dz *= f;
                     o.v[v] = (T)dz;
                 }
                 if (ACT != CPE_ACT_NONE && g.dz) store_vec<T, V>(po + at * g.ldz, o);
@@ -684,7 +782,7 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs g)
 
 // sums[n] over the workgroups' partials: 32 columns (a cache line) per
 // workgroup, 32 lanes of partials each.
-__global__ __launch_bounds__(1024) void k_column_join(GradArgs g)
+[[maybe_unused]] __global__ __launch_bounds__(1024) void k_column_join(GradArgs g)
 {
     __shared__ double lds[16][32];
     const int at = threadIdx.x & 31, n = blockIdx.x * 32 + at;
@@ -725,15 +823,21 @@ __device__ __forceinline__ int strip_swizzle(int row, int chunks)
     return chunks == 8 ? f : 2 * f;
 }
 
-template <typename T, int NT, int KT, int ACT>
+// PACKED: x and preact are rows in 8 bits, which become elements on their way
+// to LDS; where dz is rounded anyway it takes the mantissas of x's scales, and
+// dx is divided by them.
+template <typename T, int NT, int KT, int ACT, bool PACKED>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs a)
 {
+    using X = std::conditional_t<PACKED, int8_t, T>;
+    constexpr bool kFold = PACKED && folds(ACT, sizeof(T));
     constexpr int kZChunks = NT * 2, kXChunks = KT * 16;                  // chunks of an LDS row
     constexpr int kZBytes = kStripRows * kZChunks * 16, kXBytes = kStripRows * kXChunks * 16;
     constexpr int kZLoads = kStripRows * kZChunks / kNarrowThreads, kXLoads = kStripRows * kXChunks / kNarrowThreads;
     constexpr int NS = NT / 2;                                            // fragments of n
     static_assert(sizeof(T) == 2 && kZLoads >= 1, "");
     __shared__ __align__(1024) unsigned char smem[2 * (kZBytes + kXBytes)];
+    __shared__ float inverse[2][kFold ? kStripRows : 1];       // 1 / the mantissas of a strip's rows
     lds_byte *lds = (lds_byte *)smem;
     const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
     const int k_wave = (wave_base() >> 6) * 16 * KT;
@@ -761,7 +865,9 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
     const int x_col = threadIdx.x % kXChunks * 8, x_row = threadIdx.x / kXChunks;
     constexpr int kZStep = kNarrowThreads / kZChunks, kXStep = kNarrowThreads / kXChunks;
     const bool z_on = z_col < a.n, x_on = x_col < a.k && a.dw;
-    Vec<T, 8> vd[kZLoads], vz[kZLoads], vx[kXLoads];
+    Vec<T, 8> vd[kZLoads];
+    Vec<X, 8> vz[kZLoads], vx[kXLoads];
+    [[maybe_unused]] float z_scale[kZLoads], z_row_scale[kZLoads], x_scale[kXLoads];
     auto fetch = [&](int strip) {
         // rows and columns that are not there repeat others, and are set to 0 later
         const int r0 = strip * kStripRows;
@@ -769,13 +875,16 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
         for (int i = 0; i < kZLoads; i++) {
             const int r = r0 + z_row + i * kZStep, rr = r < a.rows ? r : a.rows - 1, cc = z_on ? z_col : 0;
             vd[i] = load_vec<T, 8>(static_cast<const T *>(a.dy) + rr * a.ldd + cc);
-            if (ACT != CPE_ACT_NONE) vz[i] = load_vec<T, 8>(static_cast<const T *>(a.preact) + rr * a.ldp + cc);
+            if (ACT != CPE_ACT_NONE) vz[i] = load_vec<X, 8>(static_cast<const X *>(a.preact) + rr * a.ldp + cc);
+            if constexpr (PACKED && ACT != CPE_ACT_NONE) z_scale[i] = a.z_scale[rr];
+            if constexpr (kFold) z_row_scale[i] = a.x_scale[rr];
         }
         if (!a.dw) return;
 #pragma unroll
         for (int i = 0; i < kXLoads; i++) {
             const int r = r0 + x_row + i * kXStep, rr = r < a.rows ? r : a.rows - 1;
-            vx[i] = load_vec<T, 8>(static_cast<const T *>(a.x) + rr * a.ldx + (x_on ? x_col : 0));
+            vx[i] = load_vec<X, 8>(static_cast<const X *>(a.x) + rr * a.ldx + (x_on ? x_col : 0));
+            if constexpr (PACKED) x_scale[i] = a.x_scale[rr];
         }
     };
     f32x4 acc[NT][KT];
@@ -795,13 +904,24 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
         for (int i = 0; i < kZLoads; i++) {
             const int r = z_row + i * kZStep;
             const bool on = z_on && r0 + r < a.rows;
+            [[maybe_unused]] float factor = 1.0f;
+            if constexpr (kFold) {
+                factor = scale_parts<true>(z_row_scale[i]).f;
+                if (z_col == 0) inverse[turn][r] = 1.0f / factor;
+            }
             T e[8];
 #pragma unroll
             for (int v = 0; v < 8; v++) {
                 float dz = (float)vd[i].v[v];
-                if constexpr (ACT != CPE_ACT_NONE) dz *= activate_grad<ACT>((float)vz[i].v[v]);
+                if constexpr (ACT != CPE_ACT_NONE) {
+                    if constexpr (PACKED)
+                        dz *= activate_grad<ACT>((float)vz[i].v[v] * z_scale[i]);
+                    else
+                        dz *= activate_grad<ACT>((float)vz[i].v[v]);
+                }
                 dz = on ? dz : 0.0f;
                 sums[v] += dz;
+                if constexpr (kFold) dz *= factor;
                 e[v] = (T)dz;
             }
             Fragment f;
@@ -814,7 +934,15 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
             for (int i = 0; i < kXLoads; i++) {
                 const int r = x_row + i * kXStep;
                 Fragment f;
-                __builtin_memcpy(&f, &vx[i], 16);
+                if constexpr (PACKED) {
+                    const float p = scale_parts<kFold>(x_scale[i]).p;
+                    T e[8];
+#pragma unroll
+                    for (int v = 0; v < 8; v++) e[v] = scaled_byte<T>(vx[i].v[v], p);
+                    __builtin_memcpy(&f, e, 16);
+                } else {
+                    __builtin_memcpy(&f, &vx[i], 16);
+                }
                 if (!x_on || r0 + r >= a.rows) f.u = u32x4{0, 0, 0, 0};
                 *(__attribute__((address_space(3))) u32x4 *)(
                     lx + (r * kXChunks + ((x_col >> 3) ^ strip_swizzle(r, kXChunks))) * 16) = f.u;
@@ -852,6 +980,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
 #pragma unroll
             for (int t = 0; t < kStripRows / 16; t++) {
                 const int r = 16 * t + j;
+                [[maybe_unused]] const float f = kFold ? inverse[turn][r] : 1.0f;
                 Fragment fz[NS];
 #pragma unroll
                 for (int s = 0; s < NS; s++)
@@ -867,7 +996,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
 #pragma unroll
                         for (int s = 0; s < NS; s++) v = mma<T>(fw[kt + h][s], fz[s], v);
 #pragma unroll
-                        for (int i = 0; i < 4; i++) o.v[4 * h + i] = (T)v[i];
+                        for (int i = 0; i < 4; i++) o.v[4 * h + i] = (T)(kFold ? v[i] * f : v[i]);
                     }
                     const int k = k_of(kt, 4 * c);
                     if (r0 + r < a.rows && k < a.k)
@@ -905,9 +1034,10 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_grad(WholeGradArgs
 //
 // dx: 16 columns per workgroup, its waves dividing n; w's column of each lane is
 // gathered, sixteen lanes side by side.
-template <typename T, int MT, int ACT>
+template <typename T, int MT, int ACT, bool PACKED>
 __global__ __launch_bounds__(1024) void k_rows_dx(WholeGradArgs a)
 {
+    constexpr bool kFold = PACKED && folds(ACT, sizeof(T));
     __shared__ f32x4 joined[16][MT][64];
     constexpr int E = kChunk<T>, kStep = 4 * E;
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
@@ -930,13 +1060,28 @@ __global__ __launch_bounds__(1024) void k_rows_dx(WholeGradArgs a)
             const int m = 16 * t + j, here = m < a.rows ? left : 0;
             fz[t].u = load_chunk<T>(static_cast<const T *>(a.dy) + m * a.ldd + n0, here);
             if constexpr (ACT != CPE_ACT_NONE) {
-                Fragment z;
-                z.u = load_chunk<T>(static_cast<const T *>(a.preact) + m * a.ldp + n0, here);
-                T ez[E];
-                __builtin_memcpy(e, &fz[t], 16);
-                __builtin_memcpy(ez, &z, 16);
+                float z[E];
+                [[maybe_unused]] float f = 1.0f;
+                if constexpr (PACKED) {
+                    const int8_t *pz = static_cast<const int8_t *>(a.preact) + m * a.ldp + n0;
+                    const float s = here > 0 ? a.z_scale[m] : 0.0f;
+                    if (kFold && here > 0) f = scale_parts<true>(a.x_scale[m]).f;
 #pragma unroll
-                for (int i = 0; i < E; i++) e[i] = (T)((float)e[i] * activate_grad<ACT>((float)ez[i]));
+                    for (int i = 0; i < E; i++) z[i] = i < here ? (float)pz[i] * s : 0.0f;
+                } else {
+                    Fragment raw;
+                    raw.u = load_chunk<T>(static_cast<const T *>(a.preact) + m * a.ldp + n0, here);
+                    T ez[E];
+                    __builtin_memcpy(ez, &raw, 16);
+#pragma unroll
+                    for (int i = 0; i < E; i++) z[i] = (float)ez[i];
+                }
+                __builtin_memcpy(e, &fz[t], 16);
+#pragma unroll
+                for (int i = 0; i < E; i++) {
+                    const float dz = (float)e[i] * activate_grad<ACT>(z[i]);
+                    e[i] = (T)(kFold ? dz * f : dz);
+                }
                 __builtin_memcpy(&fz[t], e, 16);
             }
         }
@@ -952,6 +1097,7 @@ __global__ __launch_bounds__(1024) void k_rows_dx(WholeGradArgs a)
         const int m = 16 * wave + j, k4 = blockIdx.x * 16 + 4 * c;
         if (m < a.rows) {
             T *out = static_cast<T *>(a.dx) + m * a.lddx + k4;
+            if constexpr (kFold) v *= 1.0f / scale_parts<true>(a.x_scale[m]).f;
 #pragma unroll
             for (int i = 0; i < 4; i++)
                 if (k4 + i < a.k) out[i] = (T)v[i];
@@ -960,9 +1106,10 @@ __global__ __launch_bounds__(1024) void k_rows_dx(WholeGradArgs a)
 }
 
 // dw and dbias: 64 n by 64 k per workgroup, 16 n of them per wave.
-template <typename T, int ACT>
+template <typename T, int ACT, bool PACKED>
 __global__ __launch_bounds__(256) void k_rows_dw(WholeGradArgs a)
 {
+    constexpr bool kFold = PACKED && folds(ACT, sizeof(T));
     constexpr int E = kChunk<T>, kStep = 4 * E;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
     const int n = blockIdx.y * 64 + wave * 16 + j, k0 = blockIdx.x * 64;
@@ -978,13 +1125,19 @@ __global__ __launch_bounds__(256) void k_rows_dw(WholeGradArgs a)
         for (int i = 0; i < E; i++) {
             const int m = m0 + i;
             float dz = 0.0f;
+            [[maybe_unused]] float f = 1.0f;
             if (n_on && m < a.rows) {
                 dz = (float)static_cast<const T *>(a.dy)[m * a.ldd + n];
-                if constexpr (ACT != CPE_ACT_NONE)
-                    dz *= activate_grad<ACT>((float)static_cast<const T *>(a.preact)[m * a.ldp + n]);
+                if constexpr (ACT != CPE_ACT_NONE) {
+                    if constexpr (PACKED)
+                        dz *= activate_grad<ACT>((float)static_cast<const int8_t *>(a.preact)[m * a.ldp + n] * a.z_scale[m]);
+                    else
+                        dz *= activate_grad<ACT>((float)static_cast<const T *>(a.preact)[m * a.ldp + n]);
+                }
+                if constexpr (kFold) f = scale_parts<true>(a.x_scale[m]).f;
             }
             sum += dz;
-            e[i] = (T)dz;
+            e[i] = (T)(kFold ? dz * f : dz);
         }
         __builtin_memcpy(&fz, e, 16);
         if (!a.dw) continue;
@@ -992,8 +1145,15 @@ __global__ __launch_bounds__(256) void k_rows_dw(WholeGradArgs a)
         for (int t = 0; t < 4; t++) {
             const int k = k0 + 16 * t + j;
 #pragma unroll
-            for (int i = 0; i < E; i++)
-                e[i] = k < a.k && m0 + i < a.rows ? static_cast<const T *>(a.x)[(m0 + i) * a.ldx + k] : (T)0.0f;
+            for (int i = 0; i < E; i++) {
+                const bool there = k < a.k && m0 + i < a.rows;
+                if constexpr (PACKED)
+                    e[i] = there ? scaled_byte<T>(static_cast<const int8_t *>(a.x)[(m0 + i) * a.ldx + k],
+                                              scale_parts<kFold>(a.x_scale[m0 + i]).p)
+                                 : (T)0.0f;
+                else
+                    e[i] = there ? static_cast<const T *>(a.x)[(m0 + i) * a.ldx + k] : (T)0.0f;
+            }
             __builtin_memcpy(&fx[t], e, 16);
         }
 #pragma unroll
@@ -1029,7 +1189,7 @@ bool direct_ok(const GemmArgs &g)
     auto ok = [](const void *p, int64_t ld, int width) {     // (a tile's offsets stay in the buffer)
         return aligned_to(p, 16) && ld % E == 0 && width % E == 0 && ld < (int64_t)kBufferBytes / 2048;
     };
-    return ok(g.a, g.lda, g.a_cols ? g.m : g.k) && ok(g.b, g.ldb, g.b_cols ? g.n : g.k);
+    return ok(g.a, g.lda, g.a_cols ? g.m : g.k) && (g.b_scale || ok(g.b, g.ldb, g.b_cols ? g.n : g.k));
 }
 
 // Workgroups dividing k where the tiles alone leave half or more of the chip
@@ -1057,7 +1217,7 @@ void choose_splits(GemmArgs &g)
     g.splits = (int32_t)ceil_div(steps, each);
 }
 
-template <typename T, bool A_ACROSS, bool B_ACROSS, int ACT>
+template <typename T, bool A_ACROSS, bool B_ACROSS, int ACT, bool PACKED = false>
 hipError_t launch_tiles(GemmArgs g, hipStream_t stream)
 {
     g.tiles_m = (int32_t)ceil_div(g.m, kTile);
@@ -1065,9 +1225,9 @@ hipError_t launch_tiles(GemmArgs g, hipStream_t stream)
     choose_splits<T>(g);
     const dim3 grid(g.tiles_m * g.tiles_n * g.splits);
     if (direct_ok<T>(g))
-        hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, true, ACT>), grid, dim3(kGemmThreads), 0, stream, g);
+        hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, true, ACT, PACKED>), grid, dim3(kGemmThreads), 0, stream, g);
     else
-        hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, false, ACT>), grid, dim3(kGemmThreads), 0, stream, g);
+        hipLaunchKernelGGL((k_gemm<T, A_ACROSS, B_ACROSS, false, ACT, PACKED>), grid, dim3(kGemmThreads), 0, stream, g);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || g.splits == 1) return e;
     const int64_t quads = (int64_t)g.m * ((g.n + 3) / 4);
     if (g.splits <= 8)
@@ -1152,7 +1312,9 @@ hipError_t launch_forward(const GemmArgs &g, hipStream_t stream)
 template <typename T>
 hipError_t launch_gemm_type(const GemmArgs &all, hipStream_t stream)
 {
-    if (all.a_cols && all.b_cols) return launch_tiles<T, true, true, CPE_ACT_NONE>(all, stream);
+    if (all.a_cols && all.b_cols)
+        return all.b_scale ? launch_tiles<T, true, true, CPE_ACT_NONE, true>(all, stream)
+                           : launch_tiles<T, true, true, CPE_ACT_NONE>(all, stream);
     const int64_t tiles_n = ceil_div(all.n, kTile), most = kMaxTiles / tiles_n * kTile;
     for (int64_t m = 0; m < all.m; m += most) {
         GemmArgs g = all;
@@ -1160,6 +1322,7 @@ hipError_t launch_gemm_type(const GemmArgs &all, hipStream_t stream)
         g.out = static_cast<T *>(all.out) + m * all.ldo;
         if (all.residual) g.residual = static_cast<const T *>(all.residual) + m * all.ldr;
         if (all.preact) g.preact = static_cast<T *>(all.preact) + m * all.ldp;
+        if (all.row_scale) g.row_scale = all.row_scale + m;
         g.m = (int32_t)(all.m - m < most ? all.m - m : most);
         hipError_t e;
         if (g.b_cols)
@@ -1196,11 +1359,18 @@ hipError_t launch_grad_width(GradArgs g, hipStream_t stream)
     }
     const int64_t slabs = ceil_div(vectors, g.slab);
     const dim3 grid(g.blocks, (unsigned)slabs);
+    auto launch = [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (ACT != CPE_ACT_NONE && g.z_scale)
+            hipLaunchKernelGGL((k_act_grad<T, V, ACT, ACT != CPE_ACT_NONE>), grid, dim3(256), 0, stream, g);
+        else
+            hipLaunchKernelGGL((k_act_grad<T, V, ACT, false>), grid, dim3(256), 0, stream, g);
+    };
     switch (g.act) {
-    case CPE_ACT_RELU: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_RELU>), grid, dim3(256), 0, stream, g); break;
-    case CPE_ACT_SILU: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_SILU>), grid, dim3(256), 0, stream, g); break;
-    case CPE_ACT_GELU: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_GELU>), grid, dim3(256), 0, stream, g); break;
-    default: hipLaunchKernelGGL((k_act_grad<T, V, CPE_ACT_NONE>), grid, dim3(256), 0, stream, g); break;
+    case CPE_ACT_RELU: launch(std::integral_constant<int, CPE_ACT_RELU>{}); break;
+    case CPE_ACT_SILU: launch(std::integral_constant<int, CPE_ACT_SILU>{}); break;
+    case CPE_ACT_GELU: launch(std::integral_constant<int, CPE_ACT_GELU>{}); break;
+    default: launch(std::integral_constant<int, CPE_ACT_NONE>{}); break;
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !g.sums || g.blocks == 1) return e;
     hipLaunchKernelGGL(k_column_join, dim3((unsigned)ceil_div(g.n, 32)), dim3(1024), 0, stream, g);
@@ -1253,11 +1423,18 @@ template <typename T, int NT, int KT>
 hipError_t launch_narrow_grad_size(const WholeGradArgs &a, hipStream_t stream)
 {
     const dim3 grid(a.blocks), block(kNarrowThreads);
+    auto launch = [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (a.x_scale)
+            hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, ACT, true>), grid, block, 0, stream, a);
+        else
+            hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, ACT, false>), grid, block, 0, stream, a);
+    };
     switch (a.act) {
-    case CPE_ACT_RELU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_RELU>), grid, block, 0, stream, a); break;
-    case CPE_ACT_SILU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_SILU>), grid, block, 0, stream, a); break;
-    case CPE_ACT_GELU: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_GELU>), grid, block, 0, stream, a); break;
-    default: hipLaunchKernelGGL((k_narrow_grad<T, NT, KT, CPE_ACT_NONE>), grid, block, 0, stream, a); break;
+    case CPE_ACT_RELU: launch(std::integral_constant<int, CPE_ACT_RELU>{}); break;
+    case CPE_ACT_SILU: launch(std::integral_constant<int, CPE_ACT_SILU>{}); break;
+    case CPE_ACT_GELU: launch(std::integral_constant<int, CPE_ACT_GELU>{}); break;
+    default: launch(std::integral_constant<int, CPE_ACT_NONE>{}); break;
     }
     return hipGetLastError();
 }
@@ -1282,25 +1459,31 @@ hipError_t launch_narrow_grad_type(WholeGradArgs a, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <typename T, int ACT>
-hipError_t launch_rows_grad(const WholeGradArgs &a, hipStream_t stream)
+template <typename T, int ACT, bool PACKED>
+hipError_t launch_rows_grad_form(const WholeGradArgs &a, hipStream_t stream)
 {
     if (a.dx) {
         const int steps = (int)ceil_div(a.n, 4 * kChunk<T>);
         const int waves = steps >= 64 ? 16 : steps >= 16 ? 8 : 4;
         const dim3 grid((unsigned)ceil_div(a.k, 16)), block(64 * waves);
         if (a.rows <= 16)
-            hipLaunchKernelGGL((k_rows_dx<T, 1, ACT>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((k_rows_dx<T, 1, ACT, PACKED>), grid, block, 0, stream, a);
         else if (a.rows <= 32)
-            hipLaunchKernelGGL((k_rows_dx<T, 2, ACT>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((k_rows_dx<T, 2, ACT, PACKED>), grid, block, 0, stream, a);
         else
-            hipLaunchKernelGGL((k_rows_dx<T, 4, ACT>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((k_rows_dx<T, 4, ACT, PACKED>), grid, block, 0, stream, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (!a.dw && !a.dbias) return hipSuccess;
     const dim3 grid(a.dw ? (unsigned)ceil_div(a.k, 64) : 1u, (unsigned)ceil_div(a.n, 64));
-    hipLaunchKernelGGL((k_rows_dw<T, ACT>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_rows_dw<T, ACT, PACKED>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename T, int ACT>
+hipError_t launch_rows_grad(const WholeGradArgs &a, hipStream_t stream)
+{
+    return a.x_scale ? launch_rows_grad_form<T, ACT, true>(a, stream) : launch_rows_grad_form<T, ACT, false>(a, stream);
 }
 
 template <typename T>

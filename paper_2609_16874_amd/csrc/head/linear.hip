@@ -5,6 +5,7 @@
 #include <new>
 
 #include "common.hpp"
+#include "cpe_rows8.h"
 
 using namespace cpe;
 
@@ -107,6 +108,136 @@ void plan_scratch(cpe_linear *h)
     h->ws_bytes = h->dz_at + align256((size_t)dz);
 }
 
+// x or preact of a gradient: of the dtype, or rows in 8 bits with their scales.
+struct Kept {
+    const void *p;
+    int64_t ld;
+    const float *scale;
+    size_t element;
+};
+
+bool check_kept(const Kept &t, int32_t width)
+{
+    return t.p && aligned_to(t.p, t.element) && t.ld >= width && t.ld <= (int64_t)1 << 40;
+}
+
+cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, const void *w, int64_t w_ld,
+                    const void *dy, int64_t dy_ld, Kept preact, void *dx, int64_t dx_ld, void *dw, int64_t dw_ld,
+                    float *dbias)
+{
+    const cpe_status st = check_call(h, rows);
+    if (st != CPE_OK) return st;
+    if (rows > 0 && !dx && !dw && !dbias) return CPE_ERR_INVALID_ARG;      // (a dx of no rows has no pointer)
+    if (!aligned_to(dbias, 4)) return CPE_ERR_INVALID_ARG;
+    const bool act = h->act != CPE_ACT_NONE;
+    if (rows > 0) {
+        if (!check_matrix(h, dy, dy_ld, h->out) || (act && !check_kept(preact, h->out))) return CPE_ERR_INVALID_ARG;
+        if (dx && (!check_matrix(h, w, w_ld, h->in) || !check_matrix(h, dx, dx_ld, h->in)))
+            return CPE_ERR_INVALID_ARG;
+        if (dw && !check_kept(x, h->in)) return CPE_ERR_INVALID_ARG;
+        if (dx && (dx == dy || dx == x.p || dx == w || dx == preact.p)) return CPE_ERR_INVALID_ARG;
+        if (dw && (dw == dy || dw == x.p || dw == w || dw == preact.p || dw == dx)) return CPE_ERR_INVALID_ARG;
+    }
+    if (dw && !check_matrix(h, dw, dw_ld, h->in)) return CPE_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    {
+        WholeGradArgs a{};
+        a.x = x.p;
+        a.ldx = x.ld;
+        a.x_scale = x.scale;
+        a.w = w;
+        a.ldw = w_ld;
+        a.dy = dy;
+        a.ldd = dy_ld;
+        a.preact = preact.p;
+        a.ldp = preact.ld;
+        a.z_scale = preact.scale;
+        a.dx = dx;
+        a.lddx = dx_ld;
+        a.dw = dw;
+        a.lddw = dw_ld;
+        a.dbias = dbias;
+        a.part = reinterpret_cast<float *>(h->ws);
+        a.part_sums = reinterpret_cast<float *>(h->ws + h->sums_at);
+        a.rows = rows;
+        a.n = h->out;
+        a.k = h->in;
+        a.act = h->act;
+        if (rows_grad_fits(rows, h->out, h->in, h->dtype)) {
+            const hipError_t e = h->dtype == CPE_HEAD_F32   ? launch_rows_grad_f32(a, stream)
+                                 : h->dtype == CPE_HEAD_F16 ? launch_rows_grad_f16(a, stream)
+                                                       : launch_rows_grad_bf16(a, stream);
+            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
+        }
+        if (narrow_grad_fits(rows, h->out, h->in, h->dtype)) {
+            const hipError_t e = h->dtype == CPE_HEAD_F16 ? launch_narrow_grad_f16(a, stream)
+                                                     : launch_narrow_grad_bf16(a, stream);
+            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
+        }
+    }
+    const bool fold = x.scale && folds(h->act, element_size(h->dtype));
+    const void *dz = dy;
+    int64_t dz_ld = dy_ld;
+    if (dbias || (act && rows > 0)) {
+        GradArgs a{};
+        a.dy = dy;
+        a.ldd = dy_ld;
+        a.preact = preact.p;
+        a.ldp = preact.ld;
+        a.z_scale = act ? preact.scale : nullptr;
+        a.x_scale = x.scale;
+        if (act && (dx || dw)) {
+            a.dz = h->ws + h->dz_at;
+            a.ldz = h->dz_ld;
+            dz = a.dz;
+            dz_ld = a.ldz;
+        }
+        a.part = reinterpret_cast<float *>(h->ws + h->sums_at);
+        a.sums = dbias;
+        a.rows = rows;
+        a.n = h->out;
+        a.act = h->act;
+        if (launch_grad(h, a, stream) != hipSuccess) return CPE_ERR_HIP;
+    }
+    if (dx && rows > 0) {       // dx[r][k] = sum_n dz[r][n] w[n][k]
+        GemmArgs g{};
+        g.a = dz;
+        g.lda = dz_ld;
+        g.b = w;
+        g.ldb = w_ld;
+        g.b_cols = true;
+        g.m = rows;
+        g.n = h->in;
+        g.k = h->out;
+        g.out = dx;
+        g.ldo = dx_ld;
+        g.row_scale = fold ? x.scale : nullptr;
+        g.part = reinterpret_cast<float *>(h->ws);
+        g.part_bytes = (int64_t)h->split_bytes;
+        if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
+    }
+    if (dw) {                   // dw[n][k] = sum_r dz[r][n] x[r][k]
+        GemmArgs g{};
+        g.a = dz;
+        g.lda = dz_ld;
+        g.a_cols = true;
+        g.b = x.p;
+        g.ldb = x.ld;
+        g.b_cols = true;
+        g.b_scale = x.scale;
+        g.fold = fold;
+        g.m = h->out;
+        g.n = h->in;
+        g.k = rows;
+        g.out = dw;
+        g.ldo = dw_ld;
+        g.part = reinterpret_cast<float *>(h->ws);
+        g.part_bytes = (int64_t)h->split_bytes;
+        if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
+    }
+    return CPE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -187,110 +318,20 @@ cpe_status cpe_linear_backward(cpe_linear *h, hipStream_t stream, int32_t rows, 
                                const void *w, int64_t w_ld, const void *dy, int64_t dy_ld, const void *preact,
                                int64_t preact_ld, void *dx, int64_t dx_ld, void *dw, int64_t dw_ld, float *dbias)
 {
-    const cpe_status st = check_call(h, rows);
-    if (st != CPE_OK) return st;
-    if (rows > 0 && !dx && !dw && !dbias) return CPE_ERR_INVALID_ARG;      // (a dx of no rows has no pointer)
-    if (!aligned_to(dbias, 4)) return CPE_ERR_INVALID_ARG;
-    const bool act = h->act != CPE_ACT_NONE;
-    if (rows > 0) {
-        if (!check_matrix(h, dy, dy_ld, h->out) || (act && !check_matrix(h, preact, preact_ld, h->out)))
-            return CPE_ERR_INVALID_ARG;
-        if (dx && (!check_matrix(h, w, w_ld, h->in) || !check_matrix(h, dx, dx_ld, h->in)))
-            return CPE_ERR_INVALID_ARG;
-        if (dw && !check_matrix(h, x, x_ld, h->in)) return CPE_ERR_INVALID_ARG;
-        if (dx && (dx == dy || dx == x || dx == w || dx == preact)) return CPE_ERR_INVALID_ARG;
-        if (dw && (dw == dy || dw == x || dw == w || dw == preact || dw == dx)) return CPE_ERR_INVALID_ARG;
-    }
-    if (dw && !check_matrix(h, dw, dw_ld, h->in)) return CPE_ERR_INVALID_ARG;
-    (void)hipGetLastError();
-    {
-        WholeGradArgs a{};
-        a.x = x;
-        a.ldx = x_ld;
-        a.w = w;
-        a.ldw = w_ld;
-        a.dy = dy;
-        a.ldd = dy_ld;
-        a.preact = preact;
-        a.ldp = preact_ld;
-        a.dx = dx;
-        a.lddx = dx_ld;
-        a.dw = dw;
-        a.lddw = dw_ld;
-        a.dbias = dbias;
-        a.part = reinterpret_cast<float *>(h->ws);
-        a.part_sums = reinterpret_cast<float *>(h->ws + h->sums_at);
-        a.rows = rows;
-        a.n = h->out;
-        a.k = h->in;
-        a.act = h->act;
-        if (rows_grad_fits(rows, h->out, h->in, h->dtype)) {
-            const hipError_t e = h->dtype == CPE_HEAD_F32   ? launch_rows_grad_f32(a, stream)
-                                 : h->dtype == CPE_HEAD_F16 ? launch_rows_grad_f16(a, stream)
-                                                       : launch_rows_grad_bf16(a, stream);
-            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
-        }
-        if (narrow_grad_fits(rows, h->out, h->in, h->dtype)) {
-            const hipError_t e = h->dtype == CPE_HEAD_F16 ? launch_narrow_grad_f16(a, stream)
-                                                     : launch_narrow_grad_bf16(a, stream);
-            return e == hipSuccess ? CPE_OK : CPE_ERR_HIP;
-        }
-    }
-    const void *dz = dy;
-    int64_t dz_ld = dy_ld;
-    if (dbias || (act && rows > 0)) {
-        GradArgs a{};
-        a.dy = dy;
-        a.ldd = dy_ld;
-        a.preact = preact;
-        a.ldp = preact_ld;
-        if (act && (dx || dw)) {
-            a.dz = h->ws + h->dz_at;
-            a.ldz = h->dz_ld;
-            dz = a.dz;
-            dz_ld = a.ldz;
-        }
-        a.part = reinterpret_cast<float *>(h->ws + h->sums_at);
-        a.sums = dbias;
-        a.rows = rows;
-        a.n = h->out;
-        a.act = h->act;
-        if (launch_grad(h, a, stream) != hipSuccess) return CPE_ERR_HIP;
-    }
-    if (dx && rows > 0) {       // dx[r][k] = sum_n dz[r][n] w[n][k]
-        GemmArgs g{};
-        g.a = dz;
-        g.lda = dz_ld;
-        g.b = w;
-        g.ldb = w_ld;
-        g.b_cols = true;
-        g.m = rows;
-        g.n = h->in;
-        g.k = h->out;
-        g.out = dx;
-        g.ldo = dx_ld;
-        g.part = reinterpret_cast<float *>(h->ws);
-        g.part_bytes = (int64_t)h->split_bytes;
-        if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
-    }
-    if (dw) {                   // dw[n][k] = sum_r dz[r][n] x[r][k]
-        GemmArgs g{};
-        g.a = dz;
-        g.lda = dz_ld;
-        g.a_cols = true;
-        g.b = x;
-        g.ldb = x_ld;
-        g.b_cols = true;
-        g.m = h->out;
-        g.n = h->in;
-        g.k = rows;
-        g.out = dw;
-        g.ldo = dw_ld;
-        g.part = reinterpret_cast<float *>(h->ws);
-        g.part_bytes = (int64_t)h->split_bytes;
-        if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
-    }
-    return CPE_OK;
+    const size_t element = h ? element_size(h->dtype) : 1;
+    return backward(h, stream, rows, {x, x_ld, nullptr, element}, w, w_ld, dy, dy_ld,
+                    {preact, preact_ld, nullptr, element}, dx, dx_ld, dw, dw_ld, dbias);
+}
+
+cpe_status cpe_linear_backward8(cpe_linear *h, hipStream_t stream, int32_t rows, const int8_t *q, int64_t q_ld,
+                                const float *scale, const void *w, int64_t w_ld, const void *dy, int64_t dy_ld,
+                                const int8_t *zq, int64_t zq_ld, const float *z_scale, void *dx, int64_t dx_ld,
+                                void *dw, int64_t dw_ld, float *dbias)
+{
+    if (!h || !aligned_to(scale, 4) || !aligned_to(z_scale, 4)) return CPE_ERR_INVALID_ARG;
+    if (rows > 0 && (!scale || (h->act != CPE_ACT_NONE && !z_scale))) return CPE_ERR_INVALID_ARG;
+    return backward(h, stream, rows, {q, q_ld, scale, 1}, w, w_ld, dy, dy_ld, {zq, zq_ld, z_scale, 1}, dx, dx_ld, dw,
+                    dw_ld, dbias);
 }
 
 cpe_status cpe_linear_destroy(cpe_linear *h)

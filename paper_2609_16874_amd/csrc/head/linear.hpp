@@ -36,6 +36,9 @@ struct GemmArgs {
     void *preact;                             // may be null: the value before the activation
     int64_t ldp;
     int act;
+    const float *row_scale;                   // may be null: out[m] /= the mantissa of row m's scale
+    const float *b_scale;                     // not null: B is bytes across k, with a scale for each k
+    bool fold;                                // of which A has the mantissas already
     float *part;                              // scratch of a split product: [splits][m][n rounded up to 4]
     int64_t part_bytes;
     int32_t splits, k_split;                  // splits > 1: each sums k_split of the k
@@ -47,6 +50,7 @@ struct GradArgs {
     const void *dy, *preact;
     int64_t ldd, ldp, ldz;
     void *dz;
+    const float *z_scale, *x_scale;           // not null: preact is bytes with these scales; dz is times x's mantissas
     float *part, *sums;                       // scratch [blocks][n]; out [n]
     int32_t rows, n, blocks, slab;            // workgroups along the rows, vectors of columns of each
     int act;
@@ -59,10 +63,15 @@ struct WholeGradArgs {
     int64_t ldx, ldw, ldd, ldp, lddx, lddw;
     void *dx, *dw;
     float *dbias;
+    const float *x_scale, *z_scale;           // x_scale not null: x and preact are bytes with these scales
     float *part, *part_sums;                  // scratch: [blocks][n][k], [blocks][n]
     int32_t rows, n, k, blocks;
     int act;
 };
+
+// Whether a gradient from rows in 8 bits has the mantissas of x's scales in dz:
+// where dz is rounded to 16 bits anyway, x then need not be.
+constexpr bool folds(int act, size_t element) { return element == 2 && (act == CPE_ACT_SILU || act == CPE_ACT_GELU); }
 
 hipError_t launch_gemm_f32(const GemmArgs &g, hipStream_t stream);
 hipError_t launch_gemm_f16(const GemmArgs &g, hipStream_t stream);

@@ -1,0 +1,68 @@
+// rows.hpp -- arguments of the kernels that work row by row: packing, RMS
+// norm and its gradient (private to the library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cpe_rows8.h"
+
+namespace cpe {
+
+constexpr int kRowsMaxWidth = 65536;
+constexpr int kRmsMaxChannels = 16384;
+constexpr int kRmsMaxBlocks = 1024;           // workgroups of the gradient, whose partial dgamma are joined
+constexpr float kLeastScale = 1.17549435e-38f;        // 2^-126
+
+// Workgroups that a gradient of C channels may have: their partial sums take
+// 8 MiB at most, or those of one workgroup per CU.
+inline int rms_most_blocks(int32_t channels)
+{
+    const int by_bytes = (1 << 21) / channels;
+    return by_bytes > kRmsMaxBlocks ? kRmsMaxBlocks : by_bytes < 256 ? 256 : by_bytes;
+}
+
+// h = x (+ residual, rounded), y = h rstd gamma (norm), or y = x; any of
+// h, y, y packed and rstd.
+struct RowsArgs {
+    const void *x, *residual;                 // residual may be null
+    const float *gamma;                       // may be null
+    void *sum, *y;                            // may be null
+    int8_t *q;                                // may be null, with scale
+    float *scale, *rstd;                      // rstd may be null
+    int64_t ldx, ldr, lds, ldy, ldq;
+    int32_t rows, width;
+    float eps;
+};
+
+struct UnpackArgs {
+    const int8_t *q;
+    const float *scale;
+    void *x;
+    int64_t ldq, ldx;
+    int32_t rows, width;
+};
+
+struct RmsGradArgs {
+    const void *h;                            // of the type, or 8 bits where h_scale is given
+    const float *h_scale;
+    const void *dy, *dsum;                    // dsum may be null
+    const float *gamma, *rstd;                // gamma may be null
+    void *dx;                                 // may be null
+    float *dgamma, *part;                     // may be null; scratch [blocks][width]
+    int64_t ldh, ldd, lds, ldx;
+    int32_t rows, width, blocks;
+};
+
+#define CPE_ROWS_LAUNCHES(type)                                                  \
+    hipError_t launch_pack_##type(const RowsArgs &a, hipStream_t stream);       \
+    hipError_t launch_unpack_##type(const UnpackArgs &a, hipStream_t stream);   \
+    hipError_t launch_rms_##type(const RowsArgs &a, hipStream_t stream);        \
+    hipError_t launch_rms_grad_##type(RmsGradArgs a, hipStream_t stream);
+CPE_ROWS_LAUNCHES(f32)
+CPE_ROWS_LAUNCHES(f16)
+CPE_ROWS_LAUNCHES(bf16)
+#undef CPE_ROWS_LAUNCHES
+
+}  // namespace cpe

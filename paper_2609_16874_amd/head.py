@@ -69,6 +69,18 @@ def _vector(t, n: int, name: str, device: int, dtype=torch.float32):
     return t.data_ptr()
 
 
+def _matrix(t, rows: Optional[int], width: int, name: str, device: int, dtype):
+    """(pointer, row stride) of a matrix, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    shape, strides = t.shape, t.stride()
+    if not (len(shape) == 2 and t.get_device() == device and t.dtype is dtype
+            and shape[1] == width and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
+        raise ValueError(f"{name}: wrong shape, dtype, device or feature stride")
+    ld = strides[0]
+    return t.data_ptr(), width if shape[0] <= 1 and ld < width else ld
+
+
 class GroupNorm:
     """Handle of one group norm (channels, groups, dtype, activation) for
     calls of up to ``max_samples`` samples of ``max_pixels`` pixels.  Maps are
@@ -195,14 +207,7 @@ class Linear:
 
     def _matrix(self, t, rows: Optional[int], width: int, name: str):
         """(pointer, row stride) of a matrix, (None, 0) for None."""
-        if t is None:
-            return None, 0
-        shape, strides = t.shape, t.stride()
-        if not (len(shape) == 2 and t.get_device() == self._device and t.dtype is self._torch_dtype
-                and shape[1] == width and (rows is None or shape[0] == rows) and (width == 1 or strides[1] == 1)):
-            raise ValueError(f"{name}: wrong shape, dtype, device or feature stride")
-        ld = strides[0]
-        return t.data_ptr(), width if shape[0] <= 1 and ld < width else ld
+        return _matrix(t, rows, width, name, self._device, self._torch_dtype)
 
     def forward(self, x, weight, bias, y, residual=None, preact=None, stream=None) -> int:
         """cpe_linear_forward: ``preact`` receives the value before the
@@ -233,6 +238,25 @@ class Linear:
                                              pz, z_ld, po, o_ld, pg, g_ld,
                                              _vector(dbias, n, "dbias", self._device))
 
+    def backward8(self, q, scale, weight, dy, preact_q=None, preact_scale=None, dx=None, dweight=None, dbias=None,
+                  stream=None) -> int:
+        """cpe_linear_backward8: the gradient from a checkpoint in 8 bits
+        (``rows8.pack``): the input as int8 [rows][in] ``q`` with float32
+        [rows] ``scale``, the value before the activation alike."""
+        rows, k, n, dev = q.shape[0], self.in_features, self.out_features, self._device
+        if rows >> 31:
+            raise ValueError(f"q: {rows} is no 32-bit number of rows")
+        pq, q_ld = _matrix(q, None, k, "q", dev, torch.int8)
+        pw, w_ld = self._matrix(weight, n, k, "weight")
+        pd, d_ld = self._matrix(dy, rows, n, "dy")
+        pz, z_ld = _matrix(preact_q, rows, n, "preact_q", dev, torch.int8)
+        po, o_ld = self._matrix(dx, rows, k, "dx")
+        pg, g_ld = self._matrix(dweight, n, k, "dweight")
+        return self._lib.cpe_linear_backward8(self._h, _stream(stream, dev), rows, pq, q_ld,
+                                              _vector(scale, rows, "scale", dev), pw, w_ld, pd, d_ld, pz, z_ld,
+                                              _vector(preact_scale, rows, "preact_scale", dev), po, o_ld, pg, g_ld,
+                                              _vector(dbias, n, "dbias", dev))
+
     def run(self, x, weight, bias=None, residual=None, keep=False, stream=None):
         """forward into new tensors: y, or (y, preact) where ``keep``.  Not
         recorded by autograd: tensors that require a gradient are refused while
@@ -255,6 +279,17 @@ class Linear:
         st = self.backward(x, weight, dy, preact, dx, dweight, dbias, stream)
         if st != CPE_OK:
             raise CpeError(st, "cpe_linear_backward")
+        return dx, dweight, dbias
+
+    def run_backward8(self, q, scale, weight, dy, preact_q=None, preact_scale=None, stream=None):
+        """backward8 into new tensors: (dx, dweight, dbias)."""
+        with _allocating(stream):
+            dx = torch.empty(q.shape, dtype=weight.dtype, device=q.device)
+            dweight = torch.empty(weight.shape, dtype=weight.dtype, device=q.device)
+            dbias = torch.empty(self.out_features, dtype=torch.float32, device=q.device)
+        st = self.backward8(q, scale, weight, dy, preact_q, preact_scale, dx, dweight, dbias, stream)
+        if st != CPE_OK:
+            raise CpeError(st, "cpe_linear_backward8")
         return dx, dweight, dbias
 
     def workspace_bytes(self) -> int:

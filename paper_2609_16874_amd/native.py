@@ -25,7 +25,7 @@ W_KEYS = 8192
 CENTROID_DTYPE = np.dtype([("bin_x", "<i4"), ("bin_y", "<i4"), ("x", "<f4"), ("y", "<f4"),
                            ("score", "<f8"), ("npix", "<i4"), ("reserved", "<i4")])
 
-# Every entry point declared in include/cpe_decode.h and include/cpe_head.h.
+# Every entry point declared in include/cpe_decode.h, include/cpe_head.h and include/cpe_rows8.h.
 EXPORTS = ("cpe_decode_create", "cpe_decode", "cpe_decode_ex", "cpe_decode_masks", "cpe_decode_destroy",
            "cpe_status_string", "cpe_decode_get_tables", "cpe_decode_get_histogram", "cpe_decode_workspace_bytes",
            "cpe_decode_set_stage_events", "cpe_decode_naive", "cpe_check_sqrt",
@@ -33,7 +33,10 @@ EXPORTS = ("cpe_decode_create", "cpe_decode", "cpe_decode_ex", "cpe_decode_masks
            "cpe_decode_test_search_mode", "cpe_decode_test_separate_list",
            "cpe_norm_create", "cpe_norm_forward", "cpe_norm_backward", "cpe_norm_destroy",
            "cpe_norm_workspace_bytes", "cpe_linear_create", "cpe_linear_forward", "cpe_linear_backward",
-           "cpe_linear_destroy", "cpe_linear_workspace_bytes")
+           "cpe_linear_destroy", "cpe_linear_workspace_bytes",
+           "cpe_rows8_pack", "cpe_rows8_unpack", "cpe_rms_create", "cpe_rms_forward", "cpe_rms_backward",
+           "cpe_rms_destroy", "cpe_rms_workspace_bytes", "cpe_linear8_create", "cpe_linear8_forward",
+           "cpe_linear8_destroy", "cpe_linear8_workspace_bytes", "cpe_linear_backward8")
 STAGE_EVENTS = 6
 MFMA_BINS = 32
 
@@ -125,6 +128,30 @@ def library():
         lib.cpe_linear_destroy.argtypes = [P]
         lib.cpe_linear_workspace_bytes.restype = ctypes.c_size_t
         lib.cpe_linear_workspace_bytes.argtypes = [P]
+        lib.cpe_rows8_pack.restype = i32
+        lib.cpe_rows8_pack.argtypes = [P, i32, i32, i32, P, i64, P, i64, P]
+        lib.cpe_rows8_unpack.restype = i32
+        lib.cpe_rows8_unpack.argtypes = [P, i32, i32, P, i64, P, i32, P, i64]
+        lib.cpe_rms_create.restype = i32
+        lib.cpe_rms_create.argtypes = [ctypes.POINTER(P), i32, i32, i32, ctypes.c_float]
+        lib.cpe_rms_forward.restype = i32
+        lib.cpe_rms_forward.argtypes = [P, P, i32, P, i64, P, i64, P, P, i64, P, i64, P, i64, P, P]
+        lib.cpe_rms_backward.restype = i32
+        lib.cpe_rms_backward.argtypes = [P, P, i32, P, i64, P, P, i64, P, P, P, i64, P, i64, P]
+        lib.cpe_rms_destroy.restype = i32
+        lib.cpe_rms_destroy.argtypes = [P]
+        lib.cpe_rms_workspace_bytes.restype = ctypes.c_size_t
+        lib.cpe_rms_workspace_bytes.argtypes = [P]
+        lib.cpe_linear8_create.restype = i32
+        lib.cpe_linear8_create.argtypes = [ctypes.POINTER(P), i32, i32, i32, i32, i32]
+        lib.cpe_linear8_forward.restype = i32
+        lib.cpe_linear8_forward.argtypes = [P, P, i32, P, i64, P, P, i64, P, P, P, i64, P, i64, P, i64]
+        lib.cpe_linear8_destroy.restype = i32
+        lib.cpe_linear8_destroy.argtypes = [P]
+        lib.cpe_linear8_workspace_bytes.restype = ctypes.c_size_t
+        lib.cpe_linear8_workspace_bytes.argtypes = [P]
+        lib.cpe_linear_backward8.restype = i32
+        lib.cpe_linear_backward8.argtypes = [P, P, i32, P, i64, P, P, i64, P, i64, P, i64, P, P, i64, P, i64, P]
         _lib = lib
     return _lib
 
