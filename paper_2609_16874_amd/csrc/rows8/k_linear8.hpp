@@ -10,8 +10,8 @@
 // are neighbouring n of one row m.
 //
 // The sums are whole numbers below 2^31 (65536 x 2^14), so their order does not
-// matter and splits of k join exactly.  They are rounded to binary32 once,
-// then scaled: three roundings of 2^-24 in all.
+// matter and splits of k join exactly.  They are rounded to binary32 once, then
+// scaled, twice: three roundings of 2^-24 in all, the last one with the bias.
 #pragma once
 
 #include "head/k_linear.hpp"
@@ -34,7 +34,10 @@ __device__ __forceinline__ i32x4 mma8(const Bytes16 &n, const Bytes16 &m, i32x4 
 
 // R rows by kStep8 of k of one operand, loaded by THREADS threads; DIRECT:
 // straight into LDS through a buffer descriptor, as the products of 16 bits.
-template <int R, int THREADS, bool DIRECT>
+// PAIRS: the rows of two fragments t = 0, 1 are n = 8 (r / 4) + 4 t + r % 4, which
+// leaves a lane eight neighbouring n of its row of sums; the chunks' places then
+// go by the bits of the row that eight lanes' reads span.
+template <int R, int THREADS, bool DIRECT, bool PAIRS = false>
 struct ByteOperand {
     static constexpr int kLoads = R * 8 / THREADS, kBytes = R * kStep8;
     const int8_t *base;
@@ -44,7 +47,8 @@ struct ByteOperand {
     u32x4 held[DIRECT ? 1 : kLoads];
 
     __device__ __forceinline__ static int row_of(int i) { return (i * THREADS + threadIdx.x) / 8; }
-    __device__ __forceinline__ static int chunk_of(int i) { return (threadIdx.x & 7) ^ (row_of(i) & 7); }
+    __device__ __forceinline__ static int swizzle(int r) { return PAIRS ? (r & 3) | ((r >> 3) & 1) << 2 : r & 7; }
+    __device__ __forceinline__ static int chunk_of(int i) { return (threadIdx.x & 7) ^ swizzle(row_of(i)); }
 
     __device__ __forceinline__ void init(const void *p, int64_t ld, int r0, int r_end, int k0)
     {
@@ -93,43 +97,106 @@ struct ByteOperand {
             for (int i = 0; i < kLoads; i++)
                 *(__attribute__((address_space(3))) u32x4 *)(lds + (i * THREADS + threadIdx.x) * 16) = held[i];
     }
-    // the fragment of rows r .. r+15 for the s-th half of the step
-    __device__ __forceinline__ static Bytes16 read(const lds_byte *lds, int r, int s)
+    // the t-th fragment of the rows from r on, for the s-th half of the step
+    __device__ __forceinline__ static Bytes16 read(const lds_byte *lds, int r, int t, int s)
     {
-        const int lane = threadIdx.x & 63, row = r + (lane & 15), c = (4 * s + (lane >> 4)) ^ (row & 7);
+        const int lane = threadIdx.x & 63, j = lane & 15;
+        const int row = r + (PAIRS ? 32 * (t >> 1) + 8 * (j >> 2) + 4 * (t & 1) + (j & 3) : 16 * t + j);
+        const int c = (4 * s + (lane >> 4)) ^ swizzle(row);
         Bytes16 f;
         f.u = *(const __attribute__((address_space(3))) u32x4 *)(lds + (row * 8 + c) * 16);
         return f;
     }
 };
 
-// W neighbouring sums of row m, scaled, then the epilogue of the other products.
+// W neighbouring values before the activation of row m, `left` of which exist.
 template <int ACT, typename T, int W>
-__device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, const int32_t (&sum)[W])
+__device__ __forceinline__ void finish_scaled(const GemmArgs &g, int m, int n, int left, const float (&z)[W])
 {
-    const float s = a.a_scale[m];
-    float v[W];
-    if (a.g.n - n >= W) {
-        const Vec<float, W> t = load_vec<float, W>(a.b_scale + n);
+    T *out = static_cast<T *>(g.out) + m * g.ldo + n;
+    const T *res = g.residual ? static_cast<const T *>(g.residual) + m * g.ldr + n : nullptr;
+    T *pre = g.preact ? static_cast<T *>(g.preact) + m * g.ldp + n : nullptr;
+    if (left >= W) {
+        Vec<T, W> o, r;
+        if (res) r = load_vec<T, W>(res);
+        if (pre) {
 #pragma unroll
-        for (int i = 0; i < W; i++) v[i] = (float)sum[i] * s * t.v[i];
+            for (int i = 0; i < W; i++) o.v[i] = (T)z[i];
+            store_vec<T, W>(pre, o);
+        }
+#pragma unroll
+        for (int i = 0; i < W; i++) {
+            const float y = activate<ACT>(z[i]);
+            o.v[i] = (T)(res ? y + (float)r.v[i] : y);
+        }
+        store_vec<T, W>(out, o);
     } else {
 #pragma unroll
-        for (int i = 0; i < W; i++) v[i] = n + i < a.g.n ? (float)sum[i] * s * a.b_scale[n + i] : 0.0f;
+        for (int i = 0; i < W; i++)
+            if (i < left) {
+                if (pre) pre[i] = (T)z[i];
+                out[i] = (T)(activate<ACT>(z[i]) + (res ? (float)res[i] : 0.0f));
+            }
     }
-    finish<ACT, T, W>(a.g, m, n, v);
+}
+
+// The scales and biases of W neighbouring n, `left` of which exist.
+template <int W>
+struct ColumnTerms {
+    float scale[W], bias[W];
+    __device__ __forceinline__ ColumnTerms(const Gemm8Args &a, int n, int left)
+    {
+        if (left >= W) {
+            const Vec<float, W> t = load_vec<float, W>(a.b_scale + n);
+            Vec<float, W> b;
+            if (a.g.bias) b = load_vec<float, W>(a.g.bias + n);
+#pragma unroll
+            for (int i = 0; i < W; i++) {
+                scale[i] = t.v[i];
+                bias[i] = a.g.bias ? b.v[i] : 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i++) {
+                scale[i] = i < left ? a.b_scale[n + i] : 0.0f;
+                bias[i] = a.g.bias && i < left ? a.g.bias[n + i] : 0.0f;
+            }
+        }
+    }
+};
+
+// W neighbouring sums of row m, whose scale is s.
+template <int ACT, typename T, int W>
+__device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float s, const ColumnTerms<W> &c,
+                                        const int32_t (&sum)[W])
+{
+    float z[W];
+#pragma unroll
+    for (int i = 0; i < W; i++) z[i] = fmaf((float)sum[i] * s, c.scale[i], c.bias[i]);
+    finish_scaled<ACT, T, W>(a.g, m, n, a.g.n - n, z);
 }
 
 // Tiles of TM x TN outputs, two LDS tiles of kStep8 k, WM x WN waves.  The
 // steps go as in the products of 16 bits: a step's two halves of fragments
 // alternate in registers, the waves meet once a step, and at the meeting the
-// next step's LDS tile has arrived.
-template <int TM, int TN, int WM, int WN, bool DIRECT, typename T, int ACT>
-__global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm8(Gemm8Args args)
+// next step's LDS tile has arrived.  A half's LDS reads (and the next tile's
+// loads) are spread over its multiplies: left to itself the compiler puts them
+// last, and the waves wait for them (16384 x 4096 to 4096 302 us, spread 285).
+//
+// WIDE: tiles of 256 x 256 and waves of 128 x 64, one workgroup per CU, for
+// products that fill the chip with them.  What bounds the tiles is LDS: a CU
+// reads and writes 128 KB a step of 128 x 128 and 256 KB of 256 x 256, which has
+// four times the multiplies of one and half the loads of all four.  Their sums
+// leave from the registers, a lane's eight neighbours at a time (through LDS
+// 8 us more a round of tiles); those of 128 x 128 tiles pass through LDS, so that
+// rows leave as whole lines (409,600 x 512 to 256 200 us, 212 from registers).
+template <bool WIDE, bool DIRECT, typename T, int ACT>
+__global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
 {
-    constexpr int kThreads = WM * WN * 64;
+    static_assert(DIRECT || !WIDE, "");
+    constexpr int TM = WIDE ? 256 : 128, TN = TM, WM = 2, WN = WIDE ? 4 : 2, kThreads = WM * WN * 64;
     using A = ByteOperand<TM, kThreads, DIRECT>;
-    using B = ByteOperand<TN, kThreads, DIRECT>;
+    using B = ByteOperand<TN, kThreads, DIRECT, WIDE>;
     constexpr int kStage = A::kBytes + B::kBytes, FM = TM / WM / 16, FN = TN / WN / 16;
     extern __shared__ __align__(1024) unsigned char gemm8_lds[];
     const GemmArgs &g = args.g;
@@ -176,15 +243,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm8(Gemm8Args args)
     auto read = [&](int step, int half) {
         const lds_byte *la = lds + (step & 1) * kStage, *lb = la + A::kBytes;
 #pragma unroll
-        for (int i = 0; i < FM; i++) fa[half][i] = A::read(la, wm + 16 * i, half);
+        for (int i = 0; i < FM; i++) fa[half][i] = A::read(la, wm, i, half);
 #pragma unroll
-        for (int j = 0; j < FN; j++) fb[half][j] = B::read(lb, wn + 16 * j, half);
+        for (int j = 0; j < FN; j++) fb[half][j] = B::read(lb, wn, j, half);
     };
     auto multiply = [&](int half) {
 #pragma unroll
         for (int i = 0; i < FM; i++)
 #pragma unroll
             for (int j = 0; j < FN; j++) acc[i][j] = mma8(fb[half][j], fa[half][i], acc[i][j]);
+    };
+    // one LDS read before every two multiplies, and one load where there are some
+    auto spread = [&](auto loads) __attribute__((always_inline)) {
+        if constexpr (WIDE)
+#pragma unroll
+            for (int u = 0; u < FM + FN; u++) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                if (u < decltype(loads)::value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
     };
     // (a split has one step at least)
     fetch_any(0);
@@ -199,6 +276,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm8(Gemm8Args args)
         __builtin_amdgcn_sched_barrier(0);
         read(t, 1);
         multiply(0);
+        spread(std::integral_constant<int, 0>{});
         __builtin_amdgcn_sched_barrier(0);
         commit(t + 1);
         wait_for_lds<true>();
@@ -207,6 +285,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm8(Gemm8Args args)
         fetch(std::false_type{}, t + 2);
         read(t + 1, 0);
         multiply(1);
+        spread(std::integral_constant<int, A::kLoads + B::kLoads>{});
         __builtin_amdgcn_sched_barrier(0);
     }
     for (; t < steps; t++) {
@@ -220,34 +299,165 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm8(Gemm8Args args)
         if (more) read(t + 1, 0);
         multiply(1);
     }
+    if constexpr (WIDE) {       // (never split)
+        const int row = lane & 15, group = lane >> 4;
+        float s[FM];
+#pragma unroll
+        for (int i = 0; i < FM; i++) {
+            const int m = m0 + wm + 16 * i + row;
+            s[i] = args.a_scale[m < g.m ? m : g.m - 1];
+        }
+#pragma unroll
+        for (int p = 0; p < FN / 2; p++) {
+            const int n = n0 + wn + 32 * p + 8 * group;
+            if (n >= g.n) continue;
+            const ColumnTerms<8> c(args, n, g.n - n);
+#pragma unroll
+            for (int i = 0; i < FM; i++) {
+                const int m = m0 + wm + 16 * i + row;
+                const i32x4 v0 = acc[i][2 * p], v1 = acc[i][2 * p + 1];
+                const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                if (m < g.m) finish8<ACT, T, 8>(args, m, n, s[i], c, v);
+            }
+        }
+        return;
+    }
     // no load is in flight, and every wave has read its last fragments: the sums
-    // pass through LDS, 128 x 128 of them at a time, so that rows leave as whole lines
+    // pass through LDS
     typedef __attribute__((address_space(3))) i32x4 lds_quad;
     auto place = [&](int m, int n) { return (lds_quad *)(lds + (m * (TN / 4) + ((n >> 2) ^ (m & 15))) * 16); };
-    constexpr int kPassRows = 2 * kStage / (TN * 4) < TM ? 2 * kStage / (TN * 4) : TM;      // that LDS holds
-    static_assert(TM % kPassRows == 0 && kPassRows % (TM / WM) == 0, "");
+    static_assert(WIDE || TM * TN * 4 <= 2 * kStage, "");
     const int64_t ldpart = (g.n + 3) / 4 * 4;
-#pragma unroll 1
-    for (int p = 0; p < TM; p += kPassRows) {
-        if (p > 0) __syncthreads();
-        if (wm >= p && wm < p + kPassRows)
 #pragma unroll
-            for (int i = 0; i < FM; i++)
+    for (int i = 0; i < FM; i++)
 #pragma unroll
-                for (int j = 0; j < FN; j++)
-                    *place(wm - p + 16 * i + (lane & 15), wn + 16 * j + 4 * (lane >> 4)) = acc[i][j];
-        __syncthreads();
-        for (int q = threadIdx.x; q < kPassRows * TN / 8; q += kThreads) {
-            const int r = q / (TN / 8), c = q % (TN / 8) * 8, m = m0 + p + r, n = n0 + c;
-            if (m >= g.m || n >= g.n) continue;
-            const i32x4 v0 = *place(r, c), v1 = *place(r, c + 4);
-            if (g.splits > 1) {
-                int32_t *to = reinterpret_cast<int32_t *>(g.part) + ((int64_t)split * g.m + m) * ldpart + n;
-                *reinterpret_cast<i32x4 *>(to) = v0;
-                if (n + 4 < g.n) *reinterpret_cast<i32x4 *>(to + 4) = v1;
-            } else {
-                const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                finish8<ACT, T, 8>(args, m, n, v);
+        for (int j = 0; j < FN; j++) *place(wm + 16 * i + (lane & 15), wn + 16 * j + 4 * (lane >> 4)) = acc[i][j];
+    __syncthreads();
+    for (int q = threadIdx.x; q < TM * TN / 8; q += kThreads) {
+        const int r = q / (TN / 8), c = q % (TN / 8) * 8, m = m0 + r, n = n0 + c;
+        if (m >= g.m || n >= g.n) continue;
+        const i32x4 v0 = *place(r, c), v1 = *place(r, c + 4);
+        if (g.splits > 1) {
+            int32_t *to = reinterpret_cast<int32_t *>(g.part) + ((int64_t)split * g.m + m) * ldpart + n;
+            *reinterpret_cast<i32x4 *>(to) = v0;
+            if (n + 4 < g.n) *reinterpret_cast<i32x4 *>(to + 4) = v1;
+        } else {
+            const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            finish8<ACT, T, 8>(args, m, n, args.a_scale[m], ColumnTerms<8>(args, n, g.n - n), v);
+        }
+    }
+}
+
+// Narrow products (a map's projection to its embedding), whose B fits into LDS
+// whole, as those of 16 bits: B is laid out once per workgroup, strips of 64 MT
+// rows of A stream past it, each read once, in whole lines, with the next strip's
+// loads in flight.
+constexpr int narrow8_bytes(int n, int ks) { return (n + 31) / 32 * 32 * ks * 64; }
+
+// FULL: k fills the fragments.  Otherwise a row's last chunk is its last 16
+// bytes, those that the chunk before has too masked to 0, and chunks beyond it
+// are 0.
+template <int KS, bool FULL, typename T, int ACT>
+__global__ __launch_bounds__(256, KS < 16 ? 2 : 1) void k_gemm8_narrow(Gemm8Args args)      // (16: LDS holds one)
+{
+    extern __shared__ __align__(1024) unsigned char gemm8_lds[];
+    const GemmArgs &g = args.g;
+    constexpr int kRow = KS * 4;        // chunks in a row of A or B
+    constexpr int MT = narrow_tiles(KS), kRows = 64 * MT, kLoads = kRows * kRow / 256, kStep = 256 / kRow;
+    lds_byte *strip_lds = (lds_byte *)gemm8_lds, *lds = strip_lds + narrow_strip_bytes(KS);
+    const int pairs = (g.n + 31) / 32, n_pad = pairs * 32;
+    // the first byte of chunk c, and how many of its bytes are not its own
+    auto start = [&](int c) { return FULL || c * 16 <= g.k - 16 ? c * 16 : g.k - 16; };
+    auto extra = [&](int c) { return c * 16 - start(c); };
+    auto masked = [&](Bytes16 f, int skip) {
+        if constexpr (!FULL)
+#pragma unroll
+            for (int d = 0; d < 4; d++) {
+                const int gone = skip - 4 * d;
+                f.u[d] &= gone <= 0 ? 0xffffffffu : gone >= 4 ? 0u : 0xffffffffu << (8 * gone);
+            }
+        return f;
+    };
+    for (int q = threadIdx.x; q < n_pad * kRow; q += 256) {
+        const int n = q / kRow, c = q % kRow;
+        Bytes16 f;
+        f.u = u32x4{0, 0, 0, 0};
+        if (n < g.n) {
+            const Vec<int8_t, 16> v = load_vec<int8_t, 16>(static_cast<const int8_t *>(g.b) + (int64_t)n * g.ldb + start(c));
+            __builtin_memcpy(&f, &v, 16);
+            f = masked(f, extra(c));
+        }
+        *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
+    }
+    const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const int row0 = (wave_base() >> 6) * 16 * MT;       // this wave's rows of a strip
+    const int strips = (int)(((int64_t)g.m + kRows - 1) / kRows);
+    const int my_chunk = threadIdx.x % kRow, my_row = threadIdx.x / kRow;
+    const int my_start = start(my_chunk), my_extra = extra(my_chunk);
+    Vec<int8_t, 16> next[kLoads];
+    auto fetch = [&](int strip) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int m = strip * kRows + my_row + i * kStep;       // (rows beyond the last repeat it)
+            next[i] = load_vec<int8_t, 16>(static_cast<const int8_t *>(g.a) + (m < g.m ? m : g.m - 1) * g.lda + my_start);
+        }
+    };
+    int strip = blockIdx.x;
+    if (strip < strips) fetch(strip);
+    const int row = 8 * (j >> 2) + (j & 3);
+    for (; strip < strips; strip += gridDim.x) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int r = my_row + i * kStep;
+            Bytes16 f;
+            __builtin_memcpy(&f, &next[i], 16);
+            f = masked(f, my_extra);
+            *(__attribute__((address_space(3))) u32x4 *)(strip_lds + (r * kRow + (my_chunk ^ (r & 7))) * 16) = f.u;
+        }
+        float s[MT];
+#pragma unroll
+        for (int t = 0; t < MT; t++) {
+            const int m = strip * kRows + row0 + 16 * t + j;
+            s[t] = args.a_scale[m < g.m ? m : g.m - 1];
+        }
+        wait_for_lds<false>();
+        meet();
+        if (strip + (int)gridDim.x < strips) fetch(strip + gridDim.x);
+        Bytes16 fa[MT][KS];
+#pragma unroll
+        for (int t = 0; t < MT; t++)
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                const int r = row0 + 16 * t + j;
+                fa[t][k].u = *(const __attribute__((address_space(3))) u32x4 *)(
+                    strip_lds + (r * kRow + ((4 * k + c) ^ (r & 7))) * 16);
+            }
+        wait_for_lds<false>();
+        meet();
+        for (int p = 0; p < pairs; p++) {
+            i32x4 acc[MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; t++) acc[t][0] = acc[t][1] = i32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const int n = 32 * p + row + 4 * h;
+                    Bytes16 fb;
+                    fb.u = *(const __attribute__((address_space(3))) u32x4 *)(
+                        lds + (n * kRow + ((4 * k + c) ^ narrow_swizzle(n))) * 16);
+#pragma unroll
+                    for (int t = 0; t < MT; t++) acc[t][h] = mma8(fb, fa[t][k], acc[t][h]);
+                }
+            const int n = 32 * p + 8 * c;
+            if (n >= g.n) continue;
+            const ColumnTerms<8> terms(args, n, g.n - n);
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                const int m = strip * kRows + row0 + 16 * t + j;
+                const int32_t v[8] = {acc[t][0][0], acc[t][0][1], acc[t][0][2], acc[t][0][3],
+                                      acc[t][1][0], acc[t][1][1], acc[t][1][2], acc[t][1][3]};
+                if (m < g.m) finish8<ACT, T, 8>(args, m, n, s[t], terms, v);
             }
         }
     }
@@ -266,7 +476,8 @@ __global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a)
     for (int s = 0; s < a.g.splits; s++) v += *reinterpret_cast<const i32x4 *>(p + s * all * 4);
     const int m = (int)(q / quads);
     const int32_t w[4] = {v[0], v[1], v[2], v[3]};
-    finish8<ACT, T, 4>(a, m, (int)(q - (int64_t)m * quads) * 4, w);
+    const int n = (int)(q - (int64_t)m * quads) * 4;
+    finish8<ACT, T, 4>(a, m, n, a.a_scale[m], ColumnTerms<4>(a, n, a.g.n - n), w);
 }
 
 // Few rows: 16 n per workgroup, its waves dividing k; fragments come straight
@@ -312,7 +523,7 @@ __global__ __launch_bounds__(1024) void k_gemm8_rows(Gemm8Args a)
         for (int w = 1; w < waves; w++) v += joined[w][wave][lane];
         const int m = 16 * wave + j, n4 = blockIdx.x * 16 + 4 * c;
         const int32_t sum[4] = {v[0], v[1], v[2], v[3]};
-        if (m < g.m && n4 < g.n) finish8<ACT, T, 4>(a, m, n4, sum);
+        if (m < g.m && n4 < g.n) finish8<ACT, T, 4>(a, m, n4, a.a_scale[m], ColumnTerms<4>(a, n4, g.n - n4), sum);
     }
 }
 
@@ -344,21 +555,74 @@ inline void choose_splits8(GemmArgs &g)
     g.splits = (int32_t)ceil_div(steps, each);
 }
 
-template <int TM, int TN, int WM, int WN, typename T, int ACT>
+// Rounds of tiles that the chip goes through: a round of wide ones (256 at
+// once) takes 1.4 to 1.85 times as long as one of the others (512 at once):
+// 7744 x 4096 to 1024 59 against 42 us, a round each; 4096^3 71 against 83, one
+// against two; 7744 x 1024 to 4096 67 against 72, two against four.
+inline bool wide8_pays(const GemmArgs &g)
+{
+    const int64_t wide = ceil_div(ceil_div(g.m, 256) * ceil_div(g.n, 256), 256);
+    const int64_t others = ceil_div(ceil_div(g.m, 128) * ceil_div(g.n, 128), 512);
+    return 10 * others > 17 * wide;
+}
+
+template <typename T, int ACT>
 hipError_t launch_tiles8(Gemm8Args a, hipStream_t stream)
 {
-    a.g.tiles_m = (int32_t)ceil_div(a.g.m, TM);
-    a.g.tiles_n = (int32_t)ceil_div(a.g.n, TN);
-    choose_splits8(a.g);
-    const dim3 grid(a.g.tiles_m * a.g.tiles_n * a.g.splits), block(WM * WN * 64);
-    constexpr int kLds = 2 * (TM + TN) * kStep8;
-    if (direct8_ok(a.g))
-        hipLaunchKernelGGL((k_gemm8<TM, TN, WM, WN, true, T, ACT>), grid, block, kLds, stream, a);
+    const bool direct = direct8_ok(a.g), wide = direct && wide8_pays(a.g);
+    const int tile = wide ? 256 : 128;
+    a.g.tiles_m = (int32_t)ceil_div(a.g.m, tile);
+    a.g.tiles_n = (int32_t)ceil_div(a.g.n, tile);
+    a.g.splits = 1;
+    a.g.k_split = a.g.k;
+    if (!wide) choose_splits8(a.g);
+    const dim3 grid(a.g.tiles_m * a.g.tiles_n * a.g.splits);
+    const int lds = 4 * tile * kStep8;
+    if (wide)
+        hipLaunchKernelGGL((k_gemm8<true, true, T, ACT>), grid, dim3(512), lds, stream, a);
+    else if (direct)
+        hipLaunchKernelGGL((k_gemm8<false, true, T, ACT>), grid, dim3(256), lds, stream, a);
     else
-        hipLaunchKernelGGL((k_gemm8<TM, TN, WM, WN, false, T, ACT>), grid, block, kLds, stream, a);
+        hipLaunchKernelGGL((k_gemm8<false, false, T, ACT>), grid, dim3(256), lds, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.g.splits == 1) return e;
     const int64_t quads = (int64_t)a.g.m * ((a.g.n + 3) / 4);
     hipLaunchKernelGGL((k_gemm8_join<T, ACT>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+// Fragments of k that hold a row (2, 4, 8 or 16), 0 where it is too long.
+inline int narrow8_steps(int k)
+{
+    for (int ks = 2; ks <= 16; ks *= 2)
+        if (k <= ks * 64) return ks;
+    return 0;
+}
+inline bool narrow8_fits(const GemmArgs &g)
+{
+    return g.k >= 16 && narrow8_steps(g.k) > 0 && g.n <= 128 && narrow8_bytes(g.n, narrow8_steps(g.k)) <= kNarrowLds;
+}
+
+template <typename T, int ACT>
+hipError_t launch_narrow8(const Gemm8Args &a, hipStream_t stream)
+{
+    // as many workgroups as run at once, by LDS and registers
+    const int ks = narrow8_steps(a.g.k), bytes = narrow8_bytes(a.g.n, ks) + narrow_strip_bytes(ks);
+    const int64_t strips = ceil_div(a.g.m, 64 * narrow_tiles(ks)), by_lds = (160 << 10) / bytes;
+    const int64_t most = 256 * (by_lds < 2 ? by_lds : 2);
+    const dim3 grid((unsigned)(strips < most ? strips : most));
+    auto launch = [&](auto steps) {
+        constexpr int KS = decltype(steps)::value;
+        if (a.g.k == KS * 64)
+            hipLaunchKernelGGL((k_gemm8_narrow<KS, true, T, ACT>), grid, dim3(256), bytes, stream, a);
+        else
+            hipLaunchKernelGGL((k_gemm8_narrow<KS, false, T, ACT>), grid, dim3(256), bytes, stream, a);
+    };
+    switch (ks) {
+    case 2: launch(std::integral_constant<int, 2>{}); break;
+    case 4: launch(std::integral_constant<int, 4>{}); break;
+    case 8: launch(std::integral_constant<int, 8>{}); break;
+    default: launch(std::integral_constant<int, 16>{}); break;
+    }
     return hipGetLastError();
 }
 
@@ -381,7 +645,8 @@ template <typename T, int ACT>
 hipError_t launch_gemm8_act(const Gemm8Args &a, hipStream_t stream)
 {
     if (a.g.m <= 16 || (a.g.m <= 64 && (int64_t)a.g.n * a.g.k <= (int64_t)1 << 23)) return launch_rows8<T, ACT>(a, stream);
-    return launch_tiles8<128, 128, 2, 2, T, ACT>(a, stream);
+    if (narrow8_fits(a.g)) return launch_narrow8<T, ACT>(a, stream);
+    return launch_tiles8<T, ACT>(a, stream);
 }
 
 // Rows in one launch: the grid stays under kMaxTiles.

@@ -27,6 +27,7 @@ SHAPES = [
     (5000, 24, 8, 0, 0), (12345, 48, 40, 0, 0), (4100, 256, 128, 0, 0), (4097, 512, 64, 16, 0), (6001, 200, 120, 0, 0),
     (9000, 136, 16, 5, 0), (5000, 304, 40, 0, 0), (2, 520, 1032, 0, 0), (33, 130, 70, 5, 0), (64, 1000, 264, 0, 0),
     (48, 96, 2500, 0, 0), (2050, 2064, 2056, 0, 0), (4100, 144, 4104, 16, 0), (700, 16384, 300, 0, 0),
+    (3900, 208, 3850, 16, 0), (8100, 16, 1900, 0, 0), (7900, 400, 2001, 0, 0), (300, 1024, 60, 0, 0), (7000, 600, 24, 1, 0),
 ]
 
 
