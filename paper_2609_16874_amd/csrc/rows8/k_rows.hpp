@@ -28,6 +28,14 @@ constexpr int row_threads() { return LANES <= 64 ? kRowThreads : LANES; }
 template <int LANES>
 constexpr int rows_at_once() { return LANES <= 64 ? kRowThreads / LANES : 1; }
 
+// Waves of a SIMD, by the elements that a thread holds: the kernels are compiled
+// for them, and the grids fill the chip with them.
+constexpr int row_waves(int lanes, int elements) { return lanes > 256 ? 4 : elements <= 8 ? 6 : elements <= 16 ? 5 : 3; }
+constexpr int grad_waves(int lanes, int elements) { return lanes > 256 ? 4 : elements <= 8 ? 5 : elements <= 16 ? 3 : 2; }
+// Whether the next row's loads are in flight with the present one's work, and
+// gamma stays (the registers of the longest rows do not hold them).
+constexpr bool row_ahead(int lanes) { return lanes <= 256; }
+
 // op over the LANES threads of a row, in a fixed order, for all of them.
 // Steps 1, 2, 4 and 8 within rows of sixteen lanes by DPP (quads permuted, then
 // mirrored halves, whose lanes are alike by then), 16 and 32 by the swaps of
@@ -75,28 +83,71 @@ __device__ __forceinline__ V row_reduce(V v, Op op, int &turn)
     return v;
 }
 
-// The vectors of a thread's share of a row: their first elements, and how many
-// of each one's elements another vector has (all where there is none).
-template <int V, int LANES, int N>
+// The vectors of a thread's share of a row: their first elements, how many of
+// each one's elements another vector has (all where there is none), and masks
+// of those that it has.
+template <typename T, int V, int LANES, int N>
 struct RowShare {
+    static constexpr int kWords = (V * (int)sizeof(T) + 3) / 4;
+    static constexpr bool kMasks = sizeof(T) < 4 && N <= 4;       // held in registers
     int at[N], extra[N];
+    bool full;                                // no element is left out, in any thread
+    uint32_t mask[kMasks ? N : 1][kWords];
     __device__ __forceinline__ RowShare(int width)
     {
         const int lane = threadIdx.x % LANES;
+        full = width == LANES * N * V;
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const int c = (lane + i * LANES) * V;
             at[i] = c + V <= width ? c : c < width ? width - V : 0;
             extra[i] = c < width ? c - at[i] : V;
+            if constexpr (kMasks)
+#pragma unroll
+                for (int w = 0; w < kWords; w++) mask[i][w] = word_mask(extra[i], w);
         }
+    }
+    __device__ __forceinline__ static uint32_t word_mask(int left_out, int w)
+    {
+        const int gone = left_out * (int)sizeof(T) - 4 * w;       // bytes of this word
+        return gone <= 0 ? 0xffffffffu : gone >= 4 ? 0u : 0xffffffffu << (8 * gone);
+    }
+    // 0 in the place of what is left out, whatever was loaded there
+    __device__ __forceinline__ Vec<T, V> own(int i, Vec<T, V> v) const
+    {
+        if (full) return v;
+        uint32_t w[kWords] = {};
+        __builtin_memcpy(w, &v, sizeof v);
+#pragma unroll
+        for (int j = 0; j < kWords; j++)
+            if constexpr (sizeof(T) == 4)
+                w[j] = j >= extra[i] ? w[j] : 0u;
+            else
+                w[j] &= kMasks ? mask[kMasks ? i : 0][j] : word_mask(extra[i], j);
+        __builtin_memcpy(&v, w, sizeof v);
+        return v;
     }
 };
 
-template <typename T, int V>
+// The elements of a vector that are this thread's; PAST: past the caches.  (A
+// whole vector is stored as one of words: from the structure the compiler makes
+// pieces of three words, one and a half, and 409,600 x 256 bytes take 100 us to
+// unpack instead of 64.)
+template <bool PAST = false, typename T, int V>
 __device__ __forceinline__ void store_own(T *p, const Vec<T, V> &v, int extra)
 {
     if (extra == 0) {
-        store_vec<T, V>(p, v);
+        if constexpr (sizeof(v) % 4 == 0) {
+            typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4), aligned(sizeof(T))));
+            words w;
+            __builtin_memcpy(&w, &v, sizeof v);
+            if constexpr (PAST)
+                __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
+            else
+                *reinterpret_cast<words *>(p) = w;
+        } else {
+            store_vec<T, V>(p, v);
+        }
         return;
     }
 #pragma unroll
@@ -104,15 +155,33 @@ __device__ __forceinline__ void store_own(T *p, const Vec<T, V> &v, int extra)
         if (i >= extra) p[i] = v.v[i];
 }
 
-// The scale s of a row whose largest |x| has these bits, and 1 / s.
+// gamma of a thread's share, in registers: loaded after the first row's loads
+template <int V, int N>
+__device__ __forceinline__ void load_gamma(const float *gamma, const int (&at)[N], float (&g)[N][V])
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        Vec<float, V> v;
+        if (gamma) v = load_vec<float, V>(gamma + at[i]);
+#pragma unroll
+        for (int e = 0; e < V; e++) g[i][e] = gamma ? v.v[e] : 1.0f;
+    }
+}
+
+// The scale s of a row whose largest |x| has these bits, and 1 / s.  Both
+// divisions are products with a reciprocal, corrected once by the remainder
+// (fma has it exactly): the division's own rounding for the scale, whose divisor
+// is a constant, and for the reciprocal to 2^-24 and a trifle.
 struct RowScale {
     float scale, inverse;
     bool bad;
     __device__ __forceinline__ explicit RowScale(uint32_t most)
     {
         bad = most >= 0x7f800000u;
-        scale = fmaxf(__builtin_bit_cast(float, most) / 127.0f, kLeastScale);
-        inverse = 1.0f / scale;
+        const float m = __builtin_bit_cast(float, most), t = m * (1.0f / 127.0f);
+        scale = fmaxf(fmaf(fmaf(-127.0f, t, m), 1.0f / 127.0f, t), kLeastScale);
+        const float r = __builtin_amdgcn_rcpf(scale);
+        inverse = fmaf(fmaf(-scale, r, 1.0f), r, r);
     }
     __device__ __forceinline__ float stored() const { return bad ? __builtin_bit_cast(float, 0x7fc00000u) : scale; }
 };
@@ -149,20 +218,13 @@ __device__ __forceinline__ Vec<int8_t, V> to_bytes(const float (&x)[V], const Ro
 }
 
 // NORM: RMS norm; otherwise y = x, packed only.
-template <typename T, int V, int LANES, int N, bool NORM>
-__global__ __launch_bounds__(row_threads<LANES>()) void k_rows(RowsArgs a)
+template <typename T, int V, int LANES, int N, bool NORM, bool PAST>
+__global__ __launch_bounds__(row_threads<LANES>(), row_waves(LANES, N *V)) void k_rows(RowsArgs a)
 {
     constexpr int R = rows_at_once<LANES>();
-    const RowShare<V, LANES, N> share(a.width);
+    const RowShare<T, V, LANES, N> share(a.width);
     const int group = LANES <= 64 ? (int)threadIdx.x / LANES : 0;
     const bool first_lane = threadIdx.x % LANES == 0;
-    float gamma[N][V];
-    if constexpr (NORM) {
-#pragma unroll
-        for (int i = 0; i < N; i++)
-#pragma unroll
-            for (int v = 0; v < V; v++) gamma[i][v] = a.gamma ? a.gamma[share.at[i] + v] : 1.0f;
-    }
     struct Raw {
         Vec<T, V> x[N], r[NORM ? N : 1];
     };
@@ -180,47 +242,52 @@ __global__ __launch_bounds__(row_threads<LANES>()) void k_rows(RowsArgs a)
     int turn = 0;
     const int64_t step = (int64_t)gridDim.x * R;
     int64_t base = (int64_t)blockIdx.x * R;
-    Raw next = fetch(base);
+    [[maybe_unused]] Raw next;
+    if constexpr (row_ahead(LANES)) next = fetch(base);
+    [[maybe_unused]] float gamma[N][V];
+    if constexpr (NORM) load_gamma<V, N>(a.gamma, share.at, gamma);
     for (; base < a.rows; base += step) {
-        const Raw raw = next;
-        if (base + step < a.rows) next = fetch(base + step);
+        const Raw raw = row_ahead(LANES) ? next : fetch(base);
+        if (row_ahead(LANES) && base + step < a.rows) next = fetch(base + step);
         const int64_t row = base + group;
         const bool on = row < a.rows;
         float h[N][V];
         [[maybe_unused]] float squares = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            Vec<T, V> o;
+            const Vec<T, V> x = share.own(i, raw.x[i]);
 #pragma unroll
-            for (int v = 0; v < V; v++) {
-                float x = (float)raw.x[i].v[v];
-                if constexpr (NORM) {
-                    if (a.residual) x = (float)rounded<T>(x + (float)raw.r[i].v[v]);
+            for (int v = 0; v < V; v++) h[i][v] = (float)x.v[v];
+            if constexpr (NORM) {
+                if (a.residual) {
+                    const Vec<T, V> r = share.own(i, raw.r[i]);
+#pragma unroll
+                    for (int v = 0; v < V; v++) h[i][v] = (float)rounded<T>(h[i][v] + (float)r.v[v]);
                 }
-                h[i][v] = v >= share.extra[i] ? x : 0.0f;
-                if constexpr (NORM) {
-                    squares = fmaf(h[i][v], h[i][v], squares);
-                    o.v[v] = (T)x;
+#pragma unroll
+                for (int v = 0; v < V; v++) squares = fmaf(h[i][v], h[i][v], squares);
+                if (a.sum && on && share.extra[i] < V) {
+                    Vec<T, V> o;
+#pragma unroll
+                    for (int v = 0; v < V; v++) o.v[v] = (T)h[i][v];
+                    store_own<PAST, T, V>(static_cast<T *>(a.sum) + row * a.lds + share.at[i], o, share.extra[i]);
                 }
             }
-            if constexpr (NORM)
-                if (a.sum && on && share.extra[i] < V)
-                    store_own<T, V>(static_cast<T *>(a.sum) + row * a.lds + share.at[i], o, share.extra[i]);
         }
         if constexpr (NORM) {
             squares = row_reduce<LANES>(squares, [](float p, float q) { return p + q; }, turn);
-            const float rstd = 1.0f / sqrtf(squares / (float)a.width + a.eps);
+            const float rstd = __builtin_amdgcn_rsqf(fmaf(squares, a.inverse_width, a.eps));
             if (a.rstd && on && first_lane) a.rstd[row] = rstd;
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                Vec<T, V> o;
 #pragma unroll
-                for (int v = 0; v < V; v++) {
-                    h[i][v] = h[i][v] * rstd * gamma[i][v];
-                    o.v[v] = (T)h[i][v];
+                for (int v = 0; v < V; v++) h[i][v] = h[i][v] * rstd * gamma[i][v];
+                if (a.y && on && share.extra[i] < V) {
+                    Vec<T, V> o;
+#pragma unroll
+                    for (int v = 0; v < V; v++) o.v[v] = (T)h[i][v];
+                    store_own<PAST, T, V>(static_cast<T *>(a.y) + row * a.ldy + share.at[i], o, share.extra[i]);
                 }
-                if (a.y && on && share.extra[i] < V)
-                    store_own<T, V>(static_cast<T *>(a.y) + row * a.ldy + share.at[i], o, share.extra[i]);
             }
         }
         if (!a.q) continue;
@@ -229,59 +296,61 @@ __global__ __launch_bounds__(row_threads<LANES>()) void k_rows(RowsArgs a)
 #pragma unroll
         for (int i = 0; i < N; i++)
 #pragma unroll
-            for (int v = 0; v < V; v++) {
-                const uint32_t b = __builtin_bit_cast(uint32_t, h[i][v]) & 0x7fffffffu;
-                // (left-out elements are 0 times what a row may hold)
-                most = v >= share.extra[i] && b > most ? b : most;
-            }
-        most = row_reduce<LANES>(most, [](uint32_t p, uint32_t q) { return p > q ? p : q; }, turn);
+            for (int v = 0; v < V; v++) most = max(most, __builtin_bit_cast(uint32_t, h[i][v]) & 0x7fffffffu);
+        most = row_reduce<LANES>(most, [](uint32_t p, uint32_t q) { return max(p, q); }, turn);
         const RowScale s(most);
         if (!on) continue;
         if (first_lane) a.scale[row] = s.stored();
 #pragma unroll
         for (int i = 0; i < N; i++)
             if (share.extra[i] < V)
-                store_own<int8_t, V>(a.q + row * a.ldq + share.at[i], to_bytes<V>(h[i], s), share.extra[i]);
+                store_own<false, int8_t, V>(a.q + row * a.ldq + share.at[i], to_bytes<V>(h[i], s), share.extra[i]);
     }
 }
 
-// x = q s.  A thread takes 16 neighbouring elements of a row (or one, of narrow
-// rows) at a time.
-template <typename T, int V>
+// x = q s.  LANES neighbouring threads take a row, eight elements each at a time
+// (or one, of narrow rows).
+template <typename T, int V, int LANES, bool PAST>
 __global__ __launch_bounds__(kRowThreads) void k_unpack(UnpackArgs a)
 {
-    const int per_row = (a.width + V - 1) / V;
-    const int64_t all = (int64_t)a.rows * per_row, step = (int64_t)gridDim.x * kRowThreads;
-    for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < all; i += step) {
-        const int64_t row = i / per_row;
-        const int c = (int)(i - row * per_row) * V, at = c + V <= a.width ? c : a.width - V;
-        const float s = a.scale[row];
-        const Vec<int8_t, V> q = load_vec<int8_t, V>(a.q + row * a.ldq + at);
-        Vec<T, V> o;
+    constexpr int R = kRowThreads / LANES, U = 4;
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const int chunk = blockIdx.y * (LANES * V) + lane * V;        // of columns
+    if (chunk >= a.width) return;
+    const int at = chunk + V <= a.width ? chunk : a.width - V, extra = chunk - at;
+    const int64_t step = (int64_t)gridDim.x * R;
+    for (int64_t r0 = (int64_t)blockIdx.x * R + group; r0 < a.rows; r0 += U * step) {
+        Vec<int8_t, V> q[U];
+        float s[U];
 #pragma unroll
-        for (int v = 0; v < V; v++) o.v[v] = scaled_byte<T>(q.v[v], s);
-        store_own<T, V>(static_cast<T *>(a.x) + row * a.ldx + at, o, c - at);
+        for (int u = 0; u < U; u++) {
+            const int64_t row = r0 + u * step < a.rows ? r0 + u * step : r0;
+            q[u] = load_vec<int8_t, V>(a.q + row * a.ldq + at);
+            s[u] = a.scale[row];
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t row = r0 + u * step;
+            if (row >= a.rows) break;
+            Vec<T, V> o;
+#pragma unroll
+            for (int v = 0; v < V; v++) o.v[v] = scaled_byte<T>(q[u].v[v], s[u]);
+            store_own<PAST, T, V>(static_cast<T *>(a.x) + row * a.ldx + at, o, extra);
+        }
     }
 }
 
 // The gradient: dx row by row, as the forward; each thread sums its columns'
 // part of dgamma over the rows that it sees, the workgroup over its threads, and
 // k_rms_join over the workgroups.
-template <typename T, int V, int LANES, int N, bool PACKED>
-__global__ __launch_bounds__(row_threads<LANES>()) void k_rms_grad(RmsGradArgs a)
+template <typename T, int V, int LANES, int N, bool PACKED, bool PAST>
+__global__ __launch_bounds__(row_threads<LANES>(), grad_waves(LANES, N *V)) void k_rms_grad(RmsGradArgs a)
 {
     using H = std::conditional_t<PACKED, int8_t, T>;
     constexpr int R = rows_at_once<LANES>();
-    const RowShare<V, LANES, N> share(a.width);
+    const RowShare<T, V, LANES, N> share(a.width);
+    const RowShare<H, V, LANES, N> h_share(a.width);
     const int group = LANES <= 64 ? (int)threadIdx.x / LANES : 0;
-    float gamma[N][V], acc[N][V];
-#pragma unroll
-    for (int i = 0; i < N; i++)
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            gamma[i][v] = a.gamma ? a.gamma[share.at[i] + v] : 1.0f;
-            acc[i][v] = 0.0f;
-        }
     struct Raw {
         Vec<H, V> h[N];
         Vec<T, V> d[N], s[N];
@@ -290,69 +359,89 @@ __global__ __launch_bounds__(row_threads<LANES>()) void k_rms_grad(RmsGradArgs a
     auto fetch = [&](int64_t base) {
         Raw raw;
         const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
-        raw.rstd = a.rstd[row];
-        raw.scale = PACKED ? a.h_scale[row] : 1.0f;
 #pragma unroll
         for (int i = 0; i < N; i++) {
             raw.h[i] = load_vec<H, V>(static_cast<const H *>(a.h) + row * a.ldh + share.at[i]);
             raw.d[i] = load_vec<T, V>(static_cast<const T *>(a.dy) + row * a.ldd + share.at[i]);
             if (a.dsum) raw.s[i] = load_vec<T, V>(static_cast<const T *>(a.dsum) + row * a.lds + share.at[i]);
         }
+        raw.rstd = a.rstd[row];
+        raw.scale = PACKED ? a.h_scale[row] : 1.0f;
         return raw;
     };
     int turn = 0;
     const int64_t step = (int64_t)gridDim.x * R;
     int64_t base = (int64_t)blockIdx.x * R;
-    Raw next{};
-    if (base < a.rows) next = fetch(base);
+    [[maybe_unused]] Raw next;
+    if (row_ahead(LANES) && base < a.rows) next = fetch(base);
+    float gamma[N][V], acc[N][V];
+    if constexpr (row_ahead(LANES)) load_gamma<V, N>(a.gamma, share.at, gamma);
+#pragma unroll
+    for (int i = 0; i < N; i++)
+#pragma unroll
+        for (int v = 0; v < V; v++) acc[i][v] = 0.0f;
     for (; base < a.rows; base += step) {
-        const Raw raw = next;
-        if (base + step < a.rows) next = fetch(base + step);
+        Raw raw = row_ahead(LANES) ? next : fetch(base);
+        if (row_ahead(LANES) && base + step < a.rows) next = fetch(base + step);
         const int64_t row = base + group;
         const bool on = row < a.rows;
+        if (base + R > a.rows && !on) {         // (a row that is not there adds nothing)
+            raw = Raw{};
+        }
+        if constexpr (!row_ahead(LANES)) load_gamma<V, N>(a.gamma, share.at, gamma);
+        const float to_xh = PACKED ? raw.scale * raw.rstd : raw.rstd;
         float xh[N][V], t[N][V], sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; i++)
+        for (int i = 0; i < N; i++) {
+            const Vec<T, V> d = share.own(i, raw.d[i]);
+            const Vec<H, V> h = h_share.own(i, raw.h[i]);
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                const bool own = on && v >= share.extra[i];
-                const float d = (float)raw.d[i].v[v], x = (float)raw.h[i].v[v];
-                xh[i][v] = (PACKED ? x * raw.scale : x) * raw.rstd;
-                t[i][v] = d * gamma[i][v];
-                sum += own ? t[i][v] * xh[i][v] : 0.0f;
-                acc[i][v] += own ? d * xh[i][v] : 0.0f;
+                xh[i][v] = (float)h.v[v] * to_xh;
+                t[i][v] = (float)d.v[v] * gamma[i][v];
+                sum = fmaf(t[i][v], xh[i][v], sum);
+                acc[i][v] = fmaf((float)d.v[v], xh[i][v], acc[i][v]);
             }
+        }
         if (!a.dx) continue;
-        sum = row_reduce<LANES>(sum, [](float p, float q) { return p + q; }, turn) / (float)a.width;
+        sum = row_reduce<LANES>(sum, [](float p, float q) { return p + q; }, turn) * a.inverse_width;
         if (!on) continue;
 #pragma unroll
         for (int i = 0; i < N; i++) {
             Vec<T, V> o;
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                float dx = raw.rstd * (t[i][v] - xh[i][v] * sum);
+                float dx = raw.rstd * fmaf(-xh[i][v], sum, t[i][v]);
                 if (a.dsum) dx += (float)raw.s[i].v[v];
                 o.v[v] = (T)dx;
             }
             if (share.extra[i] < V)
-                store_own<T, V>(static_cast<T *>(a.dx) + row * a.ldx + share.at[i], o, share.extra[i]);
+                store_own<PAST, T, V>(static_cast<T *>(a.dx) + row * a.ldx + share.at[i], o, share.extra[i]);
         }
     }
     if (!a.dgamma) return;
     float *part = a.part + (int64_t)blockIdx.x * a.width;
     if constexpr (R > 1) {
-        __shared__ float lds[R][LANES * N * V];
+        // a wave's rows' sums first, by the lanes that have the same columns
+        constexpr int kWaves = kRowThreads / 64;
+        __shared__ float lds[kWaves][LANES * N * V];
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < N; i++)
 #pragma unroll
-            for (int v = 0; v < V; v++) lds[group][(threadIdx.x % LANES + i * LANES) * V + v] = acc[i][v];
+            for (int v = 0; v < V; v++) {
+                float s = acc[i][v];
+#pragma unroll
+                for (int d = LANES; d < 64; d *= 2) s += __shfl_xor(s, d);
+                if (lane < LANES) lds[wave][(lane + i * LANES) * V + v] = s;
+            }
         __syncthreads();
         for (int c = threadIdx.x; c < a.width; c += kRowThreads) {
             // (the last vector's elements are the last V of the row)
             const int first = a.width / V * V, at = c < first || a.width % V == 0 ? c : c + (V - a.width % V);
             float s = lds[0][at];
 #pragma unroll
-            for (int r = 1; r < R; r++) s += lds[r][at];
+            for (int w = 1; w < kWaves; w++) s += lds[w][at];
             part[c] = s;
         }
     } else {
@@ -404,13 +493,13 @@ hipError_t with_row_form(int width, Call call)
     if (width < V) return call(RowForm<1, 8, 1>{});
     const int vectors = (width + V - 1) / V;
     if (vectors <= 8) return call(RowForm<V, 8, 1>{});
-    if (vectors <= 16) return call(RowForm<V, 16, 1>{});
-    if (vectors <= 32) return call(RowForm<V, 32, 1>{});
-    if (vectors <= 64) return call(RowForm<V, 64, 1>{});
+    if (vectors <= 16) return call(RowForm<V, 8, 2>{});
+    if (vectors <= 32) return call(RowForm<V, 16, 2>{});
+    if (vectors <= 64) return call(RowForm<V, 32, 2>{});
     if (vectors <= 128) return call(RowForm<V, 64, 2>{});
     if (vectors <= 256) return call(RowForm<V, 256, 1>{});
     if (vectors <= 512) return call(RowForm<V, 256, 2>{});
-    if (vectors <= 1024) return call(RowForm<V, 1024, 1>{});
+    if (vectors <= 1024) return call(RowForm<V, 512, 2>{});
     if (vectors <= 2048) return call(RowForm<V, 1024, 2>{});
     if constexpr (WIDEST > 2048)
         if (vectors <= 4096) return call(RowForm<V, 1024, 4>{});
@@ -421,53 +510,81 @@ hipError_t with_row_form(int width, Call call)
     return hipErrorInvalidValue;
 }
 
+// Whether what a call writes goes past the caches: where its rows, `bytes` for
+// each element, are more than the last cache holds, and the written ones are
+// whole lines of 16-bit values (409,600 x 256 in f16: unpacking 50 us against 64,
+// norm with y, q and rstd 98 against 101; 30,000 x 2048, which fits, norm 42
+// against 38; f32 unpacked in two stores a thread, half a line each, 55 against
+// 28).  Bytes stay in the caches, for the product that reads them next.
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;
+template <typename T>
+bool goes_past(int64_t rows, int64_t width, int64_t bytes)
+{
+    return sizeof(T) == 2 && rows * width * bytes > kCacheBytes && width % 64 == 0;
+}
+template <typename T>
+bool whole_lines(const void *p, int64_t ld) { return !p || (aligned_to(p, 128) && ld % 64 == 0); }
+
 // As many workgroups as run at once, or fewer.
 template <int LANES>
-unsigned row_blocks(int64_t rows, int64_t most)
+int64_t row_blocks(int64_t rows, int waves)
 {
-    const int64_t want = ceil_div(rows, rows_at_once<LANES>());
-    return (unsigned)(want < most ? want : most);
+    const int64_t want = ceil_div(rows, rows_at_once<LANES>()), places = 256 * (waves * 4 * 64 / row_threads<LANES>());
+    return want < places ? want : places;
 }
-constexpr int row_places(int threads) { return 256 * (2048 / threads); }
 
-template <typename T>
-hipError_t launch_pack_type(const RowsArgs &a, hipStream_t stream)
+template <typename T, bool NORM>
+hipError_t launch_rows_type(RowsArgs a, hipStream_t stream)
 {
-    return with_row_form<T, kRowsMaxWidth / kRowVec<T>>(a.width, [&](auto form) {
+    a.inverse_width = 1.0f / (float)a.width;
+    const bool past = (a.sum || a.y) &&
+                      goes_past<T>(a.rows, a.width, (1 + !!a.residual + !!a.sum + !!a.y) * (int)sizeof(T) + !!a.q) &&
+                      whole_lines<T>(a.sum, a.lds) && whole_lines<T>(a.y, a.ldy);
+    constexpr int kWidest = NORM ? kRmsMaxChannels : kRowsMaxWidth;
+    return with_row_form<T, kWidest / kRowVec<T>>(a.width, [&](auto form) {
         using F = decltype(form);
-        constexpr int kThreads = row_threads<F::LANES>();
-        const dim3 grid(row_blocks<F::LANES>(a.rows, row_places(kThreads)));
-        hipLaunchKernelGGL((k_rows<T, F::V, F::LANES, F::N, false>), grid, dim3(kThreads), 0, stream, a);
+        const dim3 grid((unsigned)row_blocks<F::LANES>(a.rows, row_waves(F::LANES, F::N * F::V)));
+        constexpr bool kPast = NORM && F::V * sizeof(T) == 16 && sizeof(T) == 2;
+        if (past)
+            hipLaunchKernelGGL((k_rows<T, F::V, F::LANES, F::N, NORM, kPast>), grid, dim3(row_threads<F::LANES>()), 0,
+                               stream, a);
+        else
+            hipLaunchKernelGGL((k_rows<T, F::V, F::LANES, F::N, NORM, false>), grid, dim3(row_threads<F::LANES>()), 0,
+                               stream, a);
         return hipGetLastError();
     });
 }
-
 template <typename T>
-hipError_t launch_rms_type(const RowsArgs &a, hipStream_t stream)
-{
-    return with_row_form<T, kRmsMaxChannels / kRowVec<T>>(a.width, [&](auto form) {
-        using F = decltype(form);
-        constexpr int kThreads = row_threads<F::LANES>();
-        const dim3 grid(row_blocks<F::LANES>(a.rows, row_places(kThreads)));
-        hipLaunchKernelGGL((k_rows<T, F::V, F::LANES, F::N, true>), grid, dim3(kThreads), 0, stream, a);
-        return hipGetLastError();
-    });
-}
+hipError_t launch_pack_type(const RowsArgs &a, hipStream_t stream) { return launch_rows_type<T, false>(a, stream); }
+template <typename T>
+hipError_t launch_rms_type(const RowsArgs &a, hipStream_t stream) { return launch_rows_type<T, true>(a, stream); }
 
 template <typename T>
 hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
 {
+    a.inverse_width = 1.0f / (float)a.width;
+    const bool past = a.dx && whole_lines<T>(a.dx, a.ldx) &&
+                      goes_past<T>(a.rows, a.width, (2 + !!a.dsum) * (int)sizeof(T) + (a.h_scale ? 1 : (int)sizeof(T)));
     const hipError_t e = with_row_form<T, kRmsMaxChannels / kRowVec<T>>(a.width, [&](auto form) {
         using F = decltype(form);
-        constexpr int kThreads = row_threads<F::LANES>();
-        const int64_t places = row_places(kThreads), most = rms_most_blocks(a.width);
+        const int64_t most = rms_most_blocks(a.width);
         // (of no rows: one workgroup, whose partial sums are 0)
-        a.blocks = (int32_t)row_blocks<F::LANES>(a.rows > 0 ? a.rows : 1, places < most ? places : most);
-        if (a.h_scale)
-            hipLaunchKernelGGL((k_rms_grad<T, F::V, F::LANES, F::N, true>), dim3(a.blocks), dim3(kThreads), 0, stream, a);
+        const int64_t blocks = row_blocks<F::LANES>(a.rows > 0 ? a.rows : 1, grad_waves(F::LANES, F::N * F::V));
+        a.blocks = (int32_t)(blocks < most ? blocks : most);
+        const dim3 grid(a.blocks), block(row_threads<F::LANES>());
+        constexpr bool kPast = F::V * sizeof(T) == 16 && sizeof(T) == 2;
+        auto launch = [&](auto packed, auto beyond) {
+            hipLaunchKernelGGL((k_rms_grad<T, F::V, F::LANES, F::N, decltype(packed)::value, decltype(beyond)::value>),
+                               grid, block, 0, stream, a);
+        };
+        if (a.h_scale && past)
+            launch(std::true_type{}, std::integral_constant<bool, kPast>{});
+        else if (a.h_scale)
+            launch(std::true_type{}, std::false_type{});
+        else if (past)
+            launch(std::false_type{}, std::integral_constant<bool, kPast>{});
         else
-            hipLaunchKernelGGL((k_rms_grad<T, F::V, F::LANES, F::N, false>), dim3(a.blocks), dim3(kThreads), 0, stream,
-                               a);
+            launch(std::false_type{}, std::false_type{});
         return hipGetLastError();
     });
     if (e != hipSuccess || !a.dgamma) return e;
@@ -478,16 +595,24 @@ hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
 template <typename T>
 hipError_t launch_unpack_type(const UnpackArgs &a, hipStream_t stream)
 {
-    auto launch = [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        const int64_t blocks = ceil_div((int64_t)a.rows * ceil_div(a.width, V), kRowThreads);
-        const int64_t most = row_places(kRowThreads);
-        hipLaunchKernelGGL((k_unpack<T, V>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(kRowThreads), 0,
-                           stream, a);
+    const bool past = goes_past<T>(a.rows, a.width, sizeof(T) + 1) && whole_lines<T>(a.x, a.ldx);
+    auto launch = [&](auto vec, auto lanes) {
+        constexpr int V = decltype(vec)::value, LANES = decltype(lanes)::value;
+        const int64_t columns = ceil_div(a.width, LANES * V), places = ceil_div(2048, columns);
+        const int64_t want = ceil_div(a.rows, kRowThreads / LANES * 4);       // (4 rows of a thread in flight)
+        const dim3 grid((unsigned)(want < places ? want : places), (unsigned)columns);
+        if (past)
+            hipLaunchKernelGGL((k_unpack<T, V, LANES, V * sizeof(T) == 16>), grid, dim3(kRowThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL((k_unpack<T, V, LANES, false>), grid, dim3(kRowThreads), 0, stream, a);
         return hipGetLastError();
     };
-    if (a.width < 8) return launch(std::integral_constant<int, 1>{});
-    return launch(std::integral_constant<int, 8>{});
+    using std::integral_constant;
+    if (a.width < 8) return launch(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    if (a.width <= 64) return launch(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    if (a.width <= 128) return launch(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+    if (a.width <= 256) return launch(integral_constant<int, 8>{}, integral_constant<int, 32>{});
+    return launch(integral_constant<int, 8>{}, integral_constant<int, 64>{});
 }
 
 }  // namespace

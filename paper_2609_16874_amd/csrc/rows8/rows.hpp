@@ -33,7 +33,7 @@ struct RowsArgs {
     float *scale, *rstd;                      // rstd may be null
     int64_t ldx, ldr, lds, ldy, ldq;
     int32_t rows, width;
-    float eps;
+    float eps, inverse_width;
 };
 
 struct UnpackArgs {
@@ -53,6 +53,7 @@ struct RmsGradArgs {
     float *dgamma, *part;                     // may be null; scratch [blocks][width]
     int64_t ldh, ldd, lds, ldx;
     int32_t rows, width, blocks;
+    float inverse_width;
 };
 
 #define CPE_ROWS_LAUNCHES(type)                                                  \
