@@ -20,15 +20,32 @@ struct __attribute__((packed, aligned(sizeof(T)))) Vec {
     T v[V];
 };
 
+// (Stored as one vector of words: from the structure the compiler makes pieces of
+// three words, one and a half where the same code stores single elements too, and
+// the stores of 16-bit rows reach two thirds of their rate.)  PAST: past the caches.
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
 {
     return *reinterpret_cast<const Vec<T, V> *>(p);
 }
+template <bool PAST = false, typename T, int V>
+__device__ __forceinline__ void store_words(T *p, const Vec<T, V> &v)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4), aligned(sizeof(T))));
+    words w;
+    __builtin_memcpy(&w, &v, sizeof v);
+    if constexpr (PAST)
+        __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
+    else
+        *reinterpret_cast<words *>(p) = w;
+}
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T *p, const Vec<T, V> &v)
 {
-    *reinterpret_cast<Vec<T, V> *>(p) = v;
+    if constexpr (sizeof(v) % 8 == 0)
+        store_words(p, v);
+    else
+        *reinterpret_cast<Vec<T, V> *>(p) = v;
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;

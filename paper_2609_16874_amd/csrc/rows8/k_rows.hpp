@@ -129,25 +129,15 @@ struct RowShare {
     }
 };
 
-// The elements of a vector that are this thread's; PAST: past the caches.  (A
-// whole vector is stored as one of words: from the structure the compiler makes
-// pieces of three words, one and a half, and 409,600 x 256 bytes take 100 us to
-// unpack instead of 64.)
+// The elements of a vector that are this thread's; PAST: past the caches.
 template <bool PAST = false, typename T, int V>
 __device__ __forceinline__ void store_own(T *p, const Vec<T, V> &v, int extra)
 {
     if (extra == 0) {
-        if constexpr (sizeof(v) % 4 == 0) {
-            typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4), aligned(sizeof(T))));
-            words w;
-            __builtin_memcpy(&w, &v, sizeof v);
-            if constexpr (PAST)
-                __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
-            else
-                *reinterpret_cast<words *>(p) = w;
-        } else {
+        if constexpr (PAST)
+            store_words<true>(p, v);
+        else
             store_vec<T, V>(p, v);
-        }
         return;
     }
 #pragma unroll
