@@ -110,7 +110,8 @@ struct ByteOperand {
 };
 
 // W neighbouring values before the activation of row m, `left` of which exist.
-template <int ACT, typename T, int W>
+// PAST: whole vectors of the outputs are stored past the caches.
+template <int ACT, bool PAST, typename T, int W>
 __device__ __forceinline__ void finish_scaled(const GemmArgs &g, int m, int n, int left, const float (&z)[W])
 {
     T *out = static_cast<T *>(g.out) + m * g.ldo + n;
@@ -122,14 +123,14 @@ __device__ __forceinline__ void finish_scaled(const GemmArgs &g, int m, int n, i
         if (pre) {
 #pragma unroll
             for (int i = 0; i < W; i++) o.v[i] = (T)z[i];
-            store_vec<T, W>(pre, o);
+            store_words<PAST>(pre, o);
         }
 #pragma unroll
         for (int i = 0; i < W; i++) {
             const float y = activate<ACT>(z[i]);
             o.v[i] = (T)(res ? y + (float)r.v[i] : y);
         }
-        store_vec<T, W>(out, o);
+        store_words<PAST>(out, o);
     } else {
 #pragma unroll
         for (int i = 0; i < W; i++)
@@ -166,14 +167,14 @@ struct ColumnTerms {
 };
 
 // W neighbouring sums of row m, whose scale is s.
-template <int ACT, typename T, int W>
+template <int ACT, bool PAST, typename T, int W>
 __device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float s, const ColumnTerms<W> &c,
                                         const int32_t (&sum)[W])
 {
     float z[W];
 #pragma unroll
     for (int i = 0; i < W; i++) z[i] = fmaf((float)sum[i] * s, c.scale[i], c.bias[i]);
-    finish_scaled<ACT, T, W>(a.g, m, n, a.g.n - n, z);
+    finish_scaled<ACT, PAST, T>(a.g, m, n, a.g.n - n, z);
 }
 
 // Tiles of TM x TN outputs, two LDS tiles of kStep8 k, WM x WN waves.  The
@@ -188,7 +189,8 @@ __device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float 
 // reads and writes 128 KB a step of 128 x 128 and 256 KB of 256 x 256, which has
 // four times the multiplies of one and half the loads of all four.  Their sums
 // leave from the registers, a lane's eight neighbours at a time (through LDS
-// 8 us more a round of tiles); those of 128 x 128 tiles pass through LDS, so that
+// 8 us more a round of tiles), past the caches, where the operands stay (with
+// a residual 277 us, 319 otherwise); those of 128 x 128 tiles pass through LDS, so that
 // rows leave as whole lines (409,600 x 512 to 256 200 us, 212 from registers).
 template <bool WIDE, bool DIRECT, typename T, int ACT>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
                 const int m = m0 + wm + 16 * i + row;
                 const i32x4 v0 = acc[i][2 * p], v1 = acc[i][2 * p + 1];
                 const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                if (m < g.m) finish8<ACT, T, 8>(args, m, n, s[i], c, v);
+                if (m < g.m) finish8<ACT, true, T>(args, m, n, s[i], c, v);
             }
         }
         return;
@@ -343,28 +345,31 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
             if (n + 4 < g.n) *reinterpret_cast<i32x4 *>(to + 4) = v1;
         } else {
             const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            finish8<ACT, T, 8>(args, m, n, args.a_scale[m], ColumnTerms<8>(args, n, g.n - n), v);
+            finish8<ACT, false, T>(args, m, n, args.a_scale[m], ColumnTerms<8>(args, n, g.n - n), v);
         }
     }
 }
 
 // Narrow products (a map's projection to its embedding), whose B fits into LDS
-// whole, as those of 16 bits: B is laid out once per workgroup, strips of 64 MT
-// rows of A stream past it, each read once, in whole lines, with the next strip's
-// loads in flight.
-constexpr int narrow8_bytes(int n, int ks) { return (n + 31) / 32 * 32 * ks * 64; }
+// whole, as those of 16 bits: B is laid out once per workgroup, strips of 64 rows
+// of A stream past it, each read once, in whole lines, with the next strip's loads
+// in flight.  Bound by memory: 409,600 x 256 to 64 in f16 31 us (5.1 TB/s) with four
+// workgroups per CU; three 33, strips of 128 rows 33 to 36 (a round of them more or
+// less is then a sixth of the work).
+constexpr int kStrip8 = 64;
+constexpr int narrow8_bytes(int n, int ks) { return ((n + 31) / 32 * 32 + kStrip8) * ks * 64; }
 
 // FULL: k fills the fragments.  Otherwise a row's last chunk is its last 16
 // bytes, those that the chunk before has too masked to 0, and chunks beyond it
 // are 0.
 template <int KS, bool FULL, typename T, int ACT>
-__global__ __launch_bounds__(256, KS < 16 ? 2 : 1) void k_gemm8_narrow(Gemm8Args args)      // (16: LDS holds one)
+__global__ __launch_bounds__(256, KS < 8 ? 4 : 2) void k_gemm8_narrow(Gemm8Args args)
 {
     extern __shared__ __align__(1024) unsigned char gemm8_lds[];
     const GemmArgs &g = args.g;
     constexpr int kRow = KS * 4;        // chunks in a row of A or B
-    constexpr int MT = narrow_tiles(KS), kRows = 64 * MT, kLoads = kRows * kRow / 256, kStep = 256 / kRow;
-    lds_byte *strip_lds = (lds_byte *)gemm8_lds, *lds = strip_lds + narrow_strip_bytes(KS);
+    constexpr int kRows = kStrip8, kLoads = kRows * kRow / 256, kStep = 256 / kRow;
+    lds_byte *strip_lds = (lds_byte *)gemm8_lds, *lds = strip_lds + kRows * KS * 64;
     const int pairs = (g.n + 31) / 32, n_pad = pairs * 32;
     // the first byte of chunk c, and how many of its bytes are not its own
     auto start = [&](int c) { return FULL || c * 16 <= g.k - 16 ? c * 16 : g.k - 16; };
@@ -390,7 +395,7 @@ __global__ __launch_bounds__(256, KS < 16 ? 2 : 1) void k_gemm8_narrow(Gemm8Args
         *(__attribute__((address_space(3))) u32x4 *)(lds + (n * kRow + (c ^ narrow_swizzle(n))) * 16) = f.u;
     }
     const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
-    const int row0 = (wave_base() >> 6) * 16 * MT;       // this wave's rows of a strip
+    const int row0 = (wave_base() >> 6) * 16;       // this wave's rows of a strip
     const int strips = (int)(((int64_t)g.m + kRows - 1) / kRows);
     const int my_chunk = threadIdx.x % kRow, my_row = threadIdx.x / kRow;
     const int my_start = start(my_chunk), my_extra = extra(my_chunk);
@@ -414,30 +419,22 @@ __global__ __launch_bounds__(256, KS < 16 ? 2 : 1) void k_gemm8_narrow(Gemm8Args
             f = masked(f, my_extra);
             *(__attribute__((address_space(3))) u32x4 *)(strip_lds + (r * kRow + (my_chunk ^ (r & 7))) * 16) = f.u;
         }
-        float s[MT];
-#pragma unroll
-        for (int t = 0; t < MT; t++) {
-            const int m = strip * kRows + row0 + 16 * t + j;
-            s[t] = args.a_scale[m < g.m ? m : g.m - 1];
-        }
+        const int m = strip * kRows + row0 + j;
+        const float s = args.a_scale[m < g.m ? m : g.m - 1];
         wait_for_lds<false>();
         meet();
         if (strip + (int)gridDim.x < strips) fetch(strip + gridDim.x);
-        Bytes16 fa[MT][KS];
+        Bytes16 fa[KS];
 #pragma unroll
-        for (int t = 0; t < MT; t++)
-#pragma unroll
-            for (int k = 0; k < KS; k++) {
-                const int r = row0 + 16 * t + j;
-                fa[t][k].u = *(const __attribute__((address_space(3))) u32x4 *)(
-                    strip_lds + (r * kRow + ((4 * k + c) ^ (r & 7))) * 16);
-            }
+        for (int k = 0; k < KS; k++) {
+            const int r = row0 + j;
+            fa[k].u = *(const __attribute__((address_space(3))) u32x4 *)(
+                strip_lds + (r * kRow + ((4 * k + c) ^ (r & 7))) * 16);
+        }
         wait_for_lds<false>();
         meet();
         for (int p = 0; p < pairs; p++) {
-            i32x4 acc[MT][2];
-#pragma unroll
-            for (int t = 0; t < MT; t++) acc[t][0] = acc[t][1] = i32x4{0, 0, 0, 0};
+            i32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
             for (int k = 0; k < KS; k++)
 #pragma unroll
@@ -446,19 +443,12 @@ __global__ __launch_bounds__(256, KS < 16 ? 2 : 1) void k_gemm8_narrow(Gemm8Args
                     Bytes16 fb;
                     fb.u = *(const __attribute__((address_space(3))) u32x4 *)(
                         lds + (n * kRow + ((4 * k + c) ^ narrow_swizzle(n))) * 16);
-#pragma unroll
-                    for (int t = 0; t < MT; t++) acc[t][h] = mma8(fb, fa[t][k], acc[t][h]);
+                    acc[h] = mma8(fb, fa[k], acc[h]);
                 }
             const int n = 32 * p + 8 * c;
-            if (n >= g.n) continue;
-            const ColumnTerms<8> terms(args, n, g.n - n);
-#pragma unroll
-            for (int t = 0; t < MT; t++) {
-                const int m = strip * kRows + row0 + 16 * t + j;
-                const int32_t v[8] = {acc[t][0][0], acc[t][0][1], acc[t][0][2], acc[t][0][3],
-                                      acc[t][1][0], acc[t][1][1], acc[t][1][2], acc[t][1][3]};
-                if (m < g.m) finish8<ACT, T, 8>(args, m, n, s[t], terms, v);
-            }
+            if (n >= g.n || m >= g.m) continue;
+            const int32_t v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+            finish8<ACT, false, T>(args, m, n, s, ColumnTerms<8>(args, n, g.n - n), v);
         }
     }
 }
@@ -477,7 +467,7 @@ __global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a)
     const int m = (int)(q / quads);
     const int32_t w[4] = {v[0], v[1], v[2], v[3]};
     const int n = (int)(q - (int64_t)m * quads) * 4;
-    finish8<ACT, T, 4>(a, m, n, a.a_scale[m], ColumnTerms<4>(a, n, a.g.n - n), w);
+    finish8<ACT, false, T>(a, m, n, a.a_scale[m], ColumnTerms<4>(a, n, a.g.n - n), w);
 }
 
 // Few rows: 16 n per workgroup, its waves dividing k; fragments come straight
@@ -523,7 +513,7 @@ __global__ __launch_bounds__(1024) void k_gemm8_rows(Gemm8Args a)
         for (int w = 1; w < waves; w++) v += joined[w][wave][lane];
         const int m = 16 * wave + j, n4 = blockIdx.x * 16 + 4 * c;
         const int32_t sum[4] = {v[0], v[1], v[2], v[3]};
-        if (m < g.m && n4 < g.n) finish8<ACT, T, 4>(a, m, n4, a.a_scale[m], ColumnTerms<4>(a, n4, g.n - n4), sum);
+        if (m < g.m && n4 < g.n) finish8<ACT, false, T>(a, m, n4, a.a_scale[m], ColumnTerms<4>(a, n4, g.n - n4), sum);
     }
 }
 
@@ -590,25 +580,21 @@ hipError_t launch_tiles8(Gemm8Args a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Fragments of k that hold a row (2, 4, 8 or 16), 0 where it is too long.
-inline int narrow8_steps(int k)
-{
-    for (int ks = 2; ks <= 16; ks *= 2)
-        if (k <= ks * 64) return ks;
-    return 0;
-}
+// Fragments of k that hold a row (2, 4 or 8), 0 where it is too long.
+inline int narrow8_steps(int k) { return k <= 128 ? 2 : k <= 256 ? 4 : k <= 512 ? 8 : 0; }
+// Where two workgroups or more fit a CU: 409,600 x 512 to 96 70 us (in tiles 85),
+// to 128, of which one fits, 122 (92).
 inline bool narrow8_fits(const GemmArgs &g)
 {
-    return g.k >= 16 && narrow8_steps(g.k) > 0 && g.n <= 128 && narrow8_bytes(g.n, narrow8_steps(g.k)) <= kNarrowLds;
+    const int ks = narrow8_steps(g.k);
+    return g.k >= 16 && ks > 0 && g.n <= 128 && 2 * narrow8_bytes(g.n, ks) <= 160 << 10;
 }
 
 template <typename T, int ACT>
 hipError_t launch_narrow8(const Gemm8Args &a, hipStream_t stream)
 {
-    // as many workgroups as run at once, by LDS and registers
-    const int ks = narrow8_steps(a.g.k), bytes = narrow8_bytes(a.g.n, ks) + narrow_strip_bytes(ks);
-    const int64_t strips = ceil_div(a.g.m, 64 * narrow_tiles(ks)), by_lds = (160 << 10) / bytes;
-    const int64_t most = 256 * (by_lds < 2 ? by_lds : 2);
+    const int ks = narrow8_steps(a.g.k), bytes = narrow8_bytes(a.g.n, ks), by_lds = (160 << 10) / bytes;
+    const int64_t strips = ceil_div(a.g.m, kStrip8), most = 256 * (by_lds < 4 ? by_lds : 4);
     const dim3 grid((unsigned)(strips < most ? strips : most));
     auto launch = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
@@ -620,8 +606,7 @@ hipError_t launch_narrow8(const Gemm8Args &a, hipStream_t stream)
     switch (ks) {
     case 2: launch(std::integral_constant<int, 2>{}); break;
     case 4: launch(std::integral_constant<int, 4>{}); break;
-    case 8: launch(std::integral_constant<int, 8>{}); break;
-    default: launch(std::integral_constant<int, 16>{}); break;
+    default: launch(std::integral_constant<int, 8>{}); break;
     }
     return hipGetLastError();
 }
