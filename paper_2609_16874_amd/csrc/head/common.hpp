@@ -117,6 +117,21 @@ __device__ __forceinline__ T rounded(float x)
 template <typename T>
 __device__ __forceinline__ T scaled_byte(int8_t q, float scale) { return rounded<T>((float)q * scale); }
 
+// A row's scale as f p: where FOLD, f is its mantissa (1 <= f < 2) and p a
+// power of two, by which bytes are exact in 16 bits; otherwise f is 1.  (So it
+// is for scales without a mantissa: 0, infinities, NaNs, subnormal ones.)
+struct ScaleParts {
+    float f, p;
+};
+template <bool FOLD>
+__device__ __forceinline__ ScaleParts scale_parts(float s)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, s);
+    const bool normal = FOLD && ((b >> 23) & 255) - 1 < 254;
+    return {normal ? __builtin_bit_cast(float, (b & 0x007fffffu) | 0x3f800000u) : 1.0f,
+            normal ? __builtin_bit_cast(float, b & 0xff800000u) : s};
+}
+
 // The work that workgroup w of n takes: workgroups are dealt to the eight XCDs
 // in turn, so this gives each XCD a run of neighbours, which share lines of
 // its L2.

@@ -90,21 +90,6 @@ __device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left)
     return f.u;
 }
 
-// A row's scale as f p: where FOLD, f is its mantissa (1 <= f < 2) and p a
-// power of two, by which bytes are exact in 16 bits; otherwise f is 1.  (So it
-// is for scales without a mantissa: 0, infinities, NaNs, subnormal ones.)
-struct ScaleParts {
-    float f, p;
-};
-template <bool FOLD>
-__device__ __forceinline__ ScaleParts scale_parts(float s)
-{
-    const uint32_t b = __builtin_bit_cast(uint32_t, s);
-    const bool normal = FOLD && ((b >> 23) & 255) - 1 < 254;
-    return {normal ? __builtin_bit_cast(float, (b & 0x007fffffu) | 0x3f800000u) : 1.0f,
-            normal ? __builtin_bit_cast(float, b & 0xff800000u) : s};
-}
-
 // One operand of a workgroup: R rows (m or n) by kStepK of k.  DIRECT: loads
 // through a buffer descriptor straight into LDS; a lane out of range has an
 // offset beyond the descriptor's, which reads as 0.
@@ -218,30 +203,32 @@ struct Operand {
 
 // An operand across k of which each k is a row in 8 bits: bytes come into
 // registers, and become elements on their way to LDS, where they lie as
-// those of Operand<T, true>.
-template <typename T>
+// those of Operand<T, true>.  RAGGED: its columns are no multiple of a chunk.
+// (Chunks of columns that are not there repeat the first one: what comes of them
+// is not stored.)
+template <typename T, bool RAGGED>
 struct PackedOperand : Operand<T, true, false> {
     using O = Operand<T, true, false>;
     static constexpr int E = O::E, kLoads = O::kLoads;
     const int8_t *from[kLoads];
     const float *scales;
     int64_t step8;
-    int columns[kLoads];
+    int columns[RAGGED ? kLoads : 1];
     Vec<int8_t, E> bytes[kLoads];
     float scale[kLoads];
-    bool fold;
+    uint32_t part;          // the bits of a scale that are taken: all, or sign and exponent
 
     __device__ __forceinline__ void init(const GemmArgs &g, int r0, int k0)
     {
         step8 = kStepK<T> * g.ldb;
         scales = g.b_scale + k0;
-        fold = g.fold;
+        part = g.fold ? 0xff800000u : 0xffffffffu;
         const int8_t *first = static_cast<const int8_t *>(g.b) + k0 * g.ldb + r0;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const int row = O::row_of(i), c = O::chunk_of(i);
-            columns[i] = g.n - r0 - c * E;
-            from[i] = first + row * g.ldb + c * E;
+            const int row = O::row_of(i), c = O::chunk_of(i), left = g.n - r0 - c * E;
+            if constexpr (RAGGED) columns[i] = left;
+            from[i] = first + row * g.ldb + (RAGGED || left > 0 ? c * E : 0);
         }
     }
     template <bool TAIL>
@@ -251,11 +238,12 @@ struct PackedOperand : Operand<T, true, false> {
         for (int i = 0; i < kLoads; i++) {
             const bool there = !TAIL || O::row_of(i) < left;
             scale[i] = there ? scales[O::row_of(i)] : 0.0f;
-            if (there && columns[i] >= E) {
+            if (there && (!RAGGED || columns[i] >= E)) {
                 bytes[i] = load_vec<int8_t, E>(from[i]);
             } else {
 #pragma unroll
-                for (int e = 0; e < E; e++) bytes[i].v[e] = there && e < columns[i] ? from[i][e] : (int8_t)0;
+                for (int e = 0; e < E; e++)
+                    bytes[i].v[e] = RAGGED && there && e < columns[RAGGED ? i : 0] ? from[i][e] : (int8_t)0;
             }
             from[i] += step8;
         }
@@ -265,7 +253,9 @@ struct PackedOperand : Operand<T, true, false> {
     {
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const float p = fold ? scale_parts<true>(scale[i]).p : scale[i];
+            // (scale_parts' p; scales without a mantissa stay whole)
+            const uint32_t b = __builtin_bit_cast(uint32_t, scale[i]);
+            const float p = __builtin_bit_cast(float, ((b >> 23) & 255) - 1 < 254 ? b & part : b);
             T e[E];
 #pragma unroll
             for (int v = 0; v < E; v++) e[v] = scaled_byte<T>(bytes[i].v[v], p);
@@ -365,11 +355,12 @@ __device__ __forceinline__ void meet()
 // (0.14).  A smaller share of LDS reads (larger tiles) gains only where no split
 // is needed; deeper staging and 32 x 32 instructions gain nothing.
 constexpr int kBand = 8;
-template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT, bool PACKED = false>
+// PACKED: B is rows in 8 bits; 1: of whole chunks, 2: ragged.
+template <typename T, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int ACT, int PACKED = 0>
 __global__ __launch_bounds__(kGemmThreads, 2) void k_gemm(GemmArgs g)
 {
     using A = Operand<T, A_ACROSS, DIRECT>;
-    using B = std::conditional_t<PACKED, PackedOperand<T>, Operand<T, B_ACROSS, DIRECT>>;
+    using B = std::conditional_t<PACKED != 0, PackedOperand<T, PACKED == 2>, Operand<T, B_ACROSS, DIRECT>>;
     constexpr int kStage = A::kBytes + B::kBytes, W = kTile / 32;       // fragments of a wave's rows
     __shared__ __align__(1024) unsigned char smem[2 * kStage];
     static_assert(2 * kStage >= kTile * kTile * 4, "the epilogue's tile fits");
@@ -1217,7 +1208,7 @@ void choose_splits(GemmArgs &g)
     g.splits = (int32_t)ceil_div(steps, each);
 }
 
-template <typename T, bool A_ACROSS, bool B_ACROSS, int ACT, bool PACKED = false>
+template <typename T, bool A_ACROSS, bool B_ACROSS, int ACT, int PACKED = 0>
 hipError_t launch_tiles(GemmArgs g, hipStream_t stream)
 {
     g.tiles_m = (int32_t)ceil_div(g.m, kTile);
@@ -1313,8 +1304,9 @@ template <typename T>
 hipError_t launch_gemm_type(const GemmArgs &all, hipStream_t stream)
 {
     if (all.a_cols && all.b_cols)
-        return all.b_scale ? launch_tiles<T, true, true, CPE_ACT_NONE, true>(all, stream)
-                           : launch_tiles<T, true, true, CPE_ACT_NONE>(all, stream);
+        return !all.b_scale                  ? launch_tiles<T, true, true, CPE_ACT_NONE>(all, stream)
+               : all.n % kChunk<T> == 0 ? launch_tiles<T, true, true, CPE_ACT_NONE, 1>(all, stream)
+                                             : launch_tiles<T, true, true, CPE_ACT_NONE, 2>(all, stream);
     const int64_t tiles_n = ceil_div(all.n, kTile), most = kMaxTiles / tiles_n * kTile;
     for (int64_t m = 0; m < all.m; m += most) {
         GemmArgs g = all;

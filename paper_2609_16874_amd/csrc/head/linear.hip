@@ -5,7 +5,7 @@
 #include <new>
 
 #include "common.hpp"
-#include "cpe_rows8.h"
+#include "rows8/rows.hpp"
 
 using namespace cpe;
 
@@ -46,6 +46,13 @@ hipError_t launch_grad(const cpe_linear *h, const GradArgs &g, hipStream_t strea
     return h->dtype == CPE_HEAD_F32   ? launch_grad_f32(g, stream)
            : h->dtype == CPE_HEAD_F16 ? launch_grad_f16(g, stream)
                                  : launch_grad_bf16(g, stream);
+}
+
+hipError_t launch_unpack(const cpe_linear *h, const UnpackArgs &u, hipStream_t stream)
+{
+    return h->dtype == CPE_HEAD_F32   ? launch_unpack_f32(u, stream)
+           : h->dtype == CPE_HEAD_F16 ? launch_unpack_f16(u, stream)
+                                 : launch_unpack_bf16(u, stream);
 }
 
 // The gradient in one pass: whole vectors of features and a dw that eight
@@ -199,7 +206,12 @@ cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, con
         a.act = h->act;
         if (launch_grad(h, a, stream) != hipSuccess) return CPE_ERR_HIP;
     }
-    if (dx && rows > 0) {       // dx[r][k] = sum_n dz[r][n] w[n][k]
+    // With many n x in 8 bits becomes x of the dtype in the place of dx, which is
+    // written after dw then: dw's tiles would convert each byte once for every 128 n
+    // (7744 x 1024 to 4096 219 us in all, 225 otherwise; 7744 x 4096 to 1024 186 and
+    // 189; 50,000 x 512 to 512 151 and 133).
+    const bool first_dw = dw && dx && rows > 0 && x.scale && h->out >= 2048;
+    auto run_dx = [&]() {       // dx[r][k] = sum_n dz[r][n] w[n][k]
         GemmArgs g{};
         g.a = dz;
         g.lda = dz_ld;
@@ -214,17 +226,31 @@ cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, con
         g.row_scale = fold ? x.scale : nullptr;
         g.part = reinterpret_cast<float *>(h->ws);
         g.part_bytes = (int64_t)h->split_bytes;
-        if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
+        return launch_gemm(h, g, stream) == hipSuccess;
+    };
+    if (first_dw) {
+        UnpackArgs u{};
+        u.q = static_cast<const int8_t *>(x.p);
+        u.ldq = x.ld;
+        u.scale = x.scale;
+        u.x = dx;
+        u.ldx = dx_ld;
+        u.rows = rows;
+        u.width = h->in;
+        u.fold = fold;
+        if (launch_unpack(h, u, stream) != hipSuccess) return CPE_ERR_HIP;
+    } else if (dx && rows > 0 && !run_dx()) {
+        return CPE_ERR_HIP;
     }
     if (dw) {                   // dw[n][k] = sum_r dz[r][n] x[r][k]
         GemmArgs g{};
         g.a = dz;
         g.lda = dz_ld;
         g.a_cols = true;
-        g.b = x.p;
-        g.ldb = x.ld;
+        g.b = first_dw ? dx : x.p;
+        g.ldb = first_dw ? dx_ld : x.ld;
         g.b_cols = true;
-        g.b_scale = x.scale;
+        g.b_scale = first_dw ? nullptr : x.scale;
         g.fold = fold;
         g.m = h->out;
         g.n = h->in;
@@ -235,6 +261,7 @@ cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, con
         g.part_bytes = (int64_t)h->split_bytes;
         if (launch_gemm(h, g, stream) != hipSuccess) return CPE_ERR_HIP;
     }
+    if (first_dw && !run_dx()) return CPE_ERR_HIP;
     return CPE_OK;
 }
 

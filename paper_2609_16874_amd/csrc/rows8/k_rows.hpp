@@ -316,7 +316,7 @@ __global__ __launch_bounds__(kRowThreads) void k_unpack(UnpackArgs a)
         for (int u = 0; u < U; u++) {
             const int64_t row = r0 + u * step < a.rows ? r0 + u * step : r0;
             q[u] = load_vec<int8_t, V>(a.q + row * a.ldq + at);
-            s[u] = a.scale[row];
+            s[u] = a.fold ? scale_parts<true>(a.scale[row]).p : a.scale[row];
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {

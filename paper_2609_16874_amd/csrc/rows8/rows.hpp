@@ -36,12 +36,14 @@ struct RowsArgs {
     float eps, inverse_width;
 };
 
+// x = q s; fold: q times the power of two of s alone (scale_parts).
 struct UnpackArgs {
     const int8_t *q;
     const float *scale;
     void *x;
     int64_t ldq, ldx;
     int32_t rows, width;
+    bool fold;
 };
 
 struct RmsGradArgs {
