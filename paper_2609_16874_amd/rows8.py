@@ -15,7 +15,7 @@ import ctypes
 
 import torch
 
-from .head import ACTIVATIONS, DTYPES, _allocating, _int32, _matrix, _need, _stream, _unrecorded, _vector
+from .head import ACTIVATIONS, DTYPES, _allocating, _int32, _matrix, _stream, _unrecorded, _vector
 from .native import CPE_OK, CpeError, library, torch_dtype
 
 _CODES = {torch.float32: DTYPES["f32"], torch.float16: DTYPES["f16"], torch.bfloat16: DTYPES["bf16"]}
@@ -24,28 +24,31 @@ _CODES = {torch.float32: DTYPES["f32"], torch.float16: DTYPES["f16"], torch.bflo
 def _packed(q, scale, rows, width, name: str, device: int):
     """(pointer, row stride, pointer of the scales) of rows in 8 bits."""
     p, ld = _matrix(q, rows, width, name, device, torch.int8)
-    return p, ld, _vector(scale, q.shape[0], f"{name}'s scale", device)
+    return p, ld, _vector(scale, q.shape[0], "the scales", device)
 
 
-def _rows(t, name: str):
-    """Rows and width of a matrix, as the C ABI's sizes; its device is the current one."""
-    _need(len(t.shape) == 2, f"{name}: a matrix is needed")
-    rows, width = t.shape
-    if rows >> 31 or width >> 31:
-        raise ValueError(f"{name}: {rows} x {width} are no 32-bit sizes")
+def _free_rows(t, name: str):
+    """(rows, width, device) of a matrix that no handle goes with, as the C
+    ABI's sizes; its device has to be the current one."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] >> 31 or shape[1] >> 31:
+        raise ValueError(f"{name}: a matrix of 32-bit sizes is needed")
     device = t.get_device()
-    _need(device >= 0 and device == torch.cuda.current_device(), f"{name}: a tensor on the current device is needed")
-    return rows, width, device
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"{name}: a tensor on the current device is needed")
+    return shape[0], shape[1], device
 
 
 def _code(dtype, name: str) -> int:
-    _need(dtype in _CODES, f"{name}: float32, float16 or bfloat16 is needed")
-    return _CODES[dtype]
+    code = _CODES.get(dtype)
+    if code is None:
+        raise ValueError(f"{name}: float32, float16 or bfloat16 is needed")
+    return code
 
 
 def pack(x, q, scale, stream=None) -> int:
     """cpe_rows8_pack: writes the rows of ``x`` in 8 bits."""
-    rows, width, dev = _rows(x, "x")
+    rows, width, dev = _free_rows(x, "x")
     code = _code(x.dtype, "x")
     px, x_ld = _matrix(x, rows, width, "x", dev, x.dtype)
     pq, q_ld, ps = _packed(q, scale, rows, width, "q", dev)
@@ -55,7 +58,7 @@ def pack(x, q, scale, stream=None) -> int:
 def unpack(q, scale, x, stream=None) -> int:
     """cpe_rows8_unpack: writes the values that rows in 8 bits stand for, in
     the type of ``x``."""
-    rows, width, dev = _rows(q, "q")
+    rows, width, dev = _free_rows(q, "q")
     code = _code(x.dtype, "x")
     px, x_ld = _matrix(x, rows, width, "x", dev, x.dtype)
     pq, q_ld, ps = _packed(q, scale, rows, width, "q", dev)
