@@ -44,11 +44,12 @@ cpe_status cpe_rows8_unpack(hipStream_t stream, int32_t rows, int32_t width, con
  * the residual stream before it:
  *   h = x, or x + residual rounded to the dtype;
  *   rstd = 1 / sqrt(sum_c h_c^2 / C + eps),  y_c = h_c rstd gamma_c.
- * The sum of squares is binary32's: where it passes 3.4e38, rstd is 0.
+ * The sum of squares is binary32's: where it passes 3.4e38, rstd is 0 (as it is
+ * for a row that holds an infinity, whose own y is then a NaN).
  *   out        receives the handle (NULL on failure)
  *   max_rows   1..2^31 - 2^23 rows of a call at most
  *   channels   C, 1..16384
- *   eps        finite, > 0
+ *   eps        finite, 2^-126 or more
  * The handle's scratch are the partial sums of dgamma: up to 8 MiB, or 256 x C
  * floats where that is more.
  */

@@ -99,7 +99,7 @@ cpe_status cpe_rms_create(cpe_rms **out, int32_t max_rows, int32_t channels, cpe
     *out = nullptr;
     if (max_rows < 1 || max_rows > kMostRows || channels < 1 || channels > kRmsMaxChannels || !is_dtype(dtype))
         return CPE_ERR_INVALID_ARG;
-    if (!std::isfinite(eps) || eps <= 0.0f) return CPE_ERR_INVALID_ARG;
+    if (!std::isfinite(eps) || eps < kLeastScale) return CPE_ERR_INVALID_ARG;
     cpe_rms *h = new (std::nothrow) cpe_rms{};
     if (!h) return CPE_ERR_OUT_OF_MEMORY;
     h->max_rows = max_rows;
@@ -142,7 +142,7 @@ cpe_status cpe_rms_forward(cpe_rms *h, hipStream_t stream, int32_t rows, const v
     if (y && (!check_rows(y, y_ld, C, element) || !in_place(y, y_ld, x, x_ld) ||
               !in_place(y, y_ld, residual, residual_ld) || y == sum))
         return CPE_ERR_INVALID_ARG;
-    if (!q != !scale) return CPE_ERR_INVALID_ARG;
+    if (!q != !scale || (scale && scale == rstd)) return CPE_ERR_INVALID_ARG;
     if (q && (!check_rows(q, q_ld, C, 1) || q == x || q == residual || q == sum || q == y))
         return CPE_ERR_INVALID_ARG;
     RowsArgs a{};

@@ -35,7 +35,7 @@ def test_no_rows_need_no_pointers():
 
 
 @pytest.mark.parametrize("change", [dict(rows=0), dict(rows=2 ** 31 - 1), dict(channels=0), dict(channels=16385),
-                                    dict(dtype=3), dict(dtype=-1), dict(eps=0.0), dict(eps=-1.0),
+                                    dict(dtype=3), dict(dtype=-1), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-39),
                                     dict(eps=float("nan")), dict(eps=float("inf"))])
 def test_rms_create_refuses(change):
     a = dict(rows=16, channels=8, dtype=1, eps=1e-6)
@@ -77,7 +77,7 @@ def test_rms_calls_refuse():
                    dict(residual_ld=7), dict(gamma=2), dict(sum=12289), dict(sum_ld=7), dict(y=16385), dict(y_ld=-8),
                    dict(q_ld=7), dict(q=None), dict(scale=None), dict(scale=24578), dict(rstd=28674), dict(y=12288),
                    dict(sum=4096, sum_ld=9), dict(sum=8192, sum_ld=9), dict(y=4096, y_ld=9), dict(y=8192, y_ld=9),
-                   dict(q=4096), dict(q=8192), dict(q=12288), dict(q=16384), dict(x_ld=2 ** 41),
+                   dict(q=4096), dict(q=8192), dict(q=12288), dict(q=16384), dict(x_ld=2 ** 41), dict(rstd=24576),
                    dict(sum=None, y=None, q=None, scale=None)):
         assert lib.cpe_rms_forward(h, None, *{**good, **change}.values()) == BAD, change
     good = dict(rows=4, h=4096, h_ld=8, h_scale=None, dy=8192, dy_ld=8, gamma=None, rstd=12288, dsum=16384, dsum_ld=8,
