@@ -11,6 +11,19 @@
 //
 // A row whose length is no multiple of V ends with its last V elements; those
 // that the vector before has too are left out of the sums and of the stores.
+//
+// A thread has sixteen elements of 16 bits (eight of 32) where the row is long
+// enough: what a row costs whatever its length (the steps of its reductions, its
+// root and quotients, about 80 instructions a wave) is shared by twice the elements
+// of one vector.  A root and two divisions of the compiler's would double it; the
+// hardware's approximations, corrected once, take their place.
+//
+// Bound by memory.  Measured (one MI355X): 409,600 x 256 in f16 packed 59 us (5.4
+// TB/s), unpacked 52 (6.0), norm to y, bytes and rstd 97 (5.4; 137 with eight
+// elements a thread and the compiler's divisions); 7744 x 1024 in bf16 with the
+// residual, its sum and bytes 11 us (5.0); the gradient of 307,039 x 100 in f32 75 us
+// (4.9) and 4 for the join of dgamma; 4096 x 16384 in f16, a workgroup of 1024 threads
+// to a row and no load ahead, 90 (4.5).
 #pragma once
 
 #include "head/common.hpp"

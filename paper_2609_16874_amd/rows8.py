@@ -27,42 +27,47 @@ def _packed(q, scale, rows, width, name: str, device: int):
     return p, ld, _vector(scale, q.shape[0], "the scales", device)
 
 
-def _free_rows(t, name: str):
-    """(rows, width, device) of a matrix that no handle goes with, as the C
-    ABI's sizes; its device has to be the current one."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] >> 31 or shape[1] >> 31:
-        raise ValueError(f"{name}: a matrix of 32-bit sizes is needed")
-    device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+def _current_device() -> int:
+    """(torch.cuda.current_device without its check that the device is set up,
+    which a tensor on it says)"""
+    return torch._C._cuda_getDevice()
+
+
+def _free_matrix(t, name: str):
+    """(pointer, row stride, rows, width, device) of a matrix that no handle
+    goes with, as the C ABI's sizes; its device has to be the current one."""
+    shape, strides, device = t.shape, t.stride(), t.get_device()
+    if len(shape) != 2 or shape[0] >> 31 or shape[1] >> 31 or (shape[1] != 1 and strides[1] != 1):
+        raise ValueError(f"{name}: a matrix of 32-bit sizes and contiguous rows is needed")
+    if device < 0 or device != _current_device():
         raise ValueError(f"{name}: a tensor on the current device is needed")
-    return shape[0], shape[1], device
-
-
-def _code(dtype, name: str) -> int:
-    code = _CODES.get(dtype)
-    if code is None:
-        raise ValueError(f"{name}: float32, float16 or bfloat16 is needed")
-    return code
+    rows, width = shape
+    ld = strides[0]
+    return t.data_ptr(), width if rows <= 1 and ld < width else ld, rows, width, device
 
 
 def pack(x, q, scale, stream=None) -> int:
     """cpe_rows8_pack: writes the rows of ``x`` in 8 bits."""
-    rows, width, dev = _free_rows(x, "x")
-    code = _code(x.dtype, "x")
-    px, x_ld = _matrix(x, rows, width, "x", dev, x.dtype)
-    pq, q_ld, ps = _packed(q, scale, rows, width, "q", dev)
-    return library().cpe_rows8_pack(_stream(stream, dev), rows, width, code, px, x_ld, pq, q_ld, ps)
+    px, x_ld, rows, width, dev = _free_matrix(x, "x")
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise ValueError("x: float32, float16 or bfloat16 is needed")
+    pq, q_ld = _matrix(q, rows, width, "q", dev, torch.int8)
+    return library().cpe_rows8_pack(_stream(stream, dev), rows, width, code, px, x_ld, pq, q_ld,
+                                    _vector(scale, rows, "scale", dev))
 
 
 def unpack(q, scale, x, stream=None) -> int:
     """cpe_rows8_unpack: writes the values that rows in 8 bits stand for, in
     the type of ``x``."""
-    rows, width, dev = _free_rows(q, "q")
-    code = _code(x.dtype, "x")
-    px, x_ld = _matrix(x, rows, width, "x", dev, x.dtype)
-    pq, q_ld, ps = _packed(q, scale, rows, width, "q", dev)
-    return library().cpe_rows8_unpack(_stream(stream, dev), rows, width, pq, q_ld, ps, code, px, x_ld)
+    pq, q_ld, rows, width, dev = _free_matrix(q, "q")
+    dtype = x.dtype
+    code = _CODES.get(dtype)
+    if code is None or q.dtype is not torch.int8:
+        raise ValueError("q: int8, and x: float32, float16 or bfloat16 are needed")
+    px, x_ld = _matrix(x, rows, width, "x", dev, dtype)
+    return library().cpe_rows8_unpack(_stream(stream, dev), rows, width, pq, q_ld, _vector(scale, rows, "scale", dev),
+                                      code, px, x_ld)
 
 
 def packed(x, stream=None):

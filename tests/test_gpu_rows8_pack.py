@@ -164,3 +164,20 @@ def test_offsets_beyond_32_bits():
     check_packed(q[-n:], scale[-n:], part.double(), 0.0)
     v = rows8().unpacked(q, scale, "bf16")
     assert torch.equal(v[-n:], (q[-n:].float() * scale[-n:, None]).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_rows_that_the_caches_do_not_hold(dtype):
+    """300,000 x 512: written past the caches, in whole lines; the same rows in
+    pieces, and in wider ones that are not, are written through them."""
+    M, C = 300_000, 512
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((M, C), generator=g, device="cuda").to(DTYPES[dtype])
+    q, scale = rows8().packed(x)
+    v = rows8().unpacked(q, scale, dtype)
+    for lo in range(0, M, 100_000):
+        part = slice(lo, lo + 100_000)
+        assert torch.equal(rows8().unpacked(q[part], scale[part], dtype), v[part])
+    wide = torch.full((M, C + 8), 77.0, dtype=DTYPES[dtype], device="cuda")
+    assert rows8().unpack(q, scale, wide[:, :C]) == 0
+    assert torch.equal(wide[:, :C], v) and bool((wide[:, C:] == 77.0).all())

@@ -258,3 +258,33 @@ def test_offsets_beyond_32_bits():
     want = 180 * (want.to(torch.bfloat16).double() * xh).sum(0)
     assert float(((dgamma.double() - want) / want).abs().max()) <= 2.0 ** -8
     norm.close()
+
+
+@pytest.mark.parametrize("C", [64, 512, 4096])
+def test_rows_that_the_caches_do_not_hold(C):
+    """150 M elements, written past the caches: the same rows in pieces, which
+    are not, give the same bits; dgamma to the sums' bound."""
+    M = (150 << 20) // C
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, res, dy = (torch.randn((M, C), generator=g, device="cuda").half() for _ in range(3))
+    gamma = 1.0 + 0.3 * matrix(1, C, "f32", 5)[0].cuda()
+    norm = rows8().RmsNorm(M, C, "f16", EPS)
+    total, y, rstd = norm.run(x, gamma, res)
+    _, (q, scale), _ = norm.run(x, gamma, res, packed=True)
+    kept, kept_scale = rows8().packed(total)
+    dx, dgamma = norm.run_backward(total, dy, gamma, rstd, res)
+    dx8, _ = norm.run_backward(kept, dy, gamma, rstd, res, kept_scale)
+    sums, most, each = 0.0, 0.0, -(-M // 5)
+    for lo in range(0, M, each):
+        p = slice(lo, min(M, lo + each))
+        t, u, r = norm.run(x[p], gamma, res[p])
+        _, (b, s), _ = norm.run(x[p], gamma, res[p], packed=True)
+        assert torch.equal(t, total[p]) and torch.equal(u, y[p]) and torch.equal(r, rstd[p])
+        assert torch.equal(b, q[p]) and torch.equal(s, scale[p])
+        d, dg = norm.run_backward(t, dy[p], gamma, r, res[p])
+        assert torch.equal(d, dx[p])
+        assert torch.equal(norm.run_backward(kept[p], dy[p], gamma, r, res[p], kept_scale[p])[0], dx8[p])
+        sums = sums + dg.double()
+        most = most + (dy[p].double() * t.double() * r.double()[:, None]).abs().sum(0)
+    assert bool(((dgamma.double() - sums).abs() <= 2 * (M + 8) * E32 * most).all())
+    norm.close()

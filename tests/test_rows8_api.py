@@ -148,7 +148,7 @@ def recorded(monkeypatch):
     from paper_2609_16874_amd import head, rows8
     lib = Recorder()
     monkeypatch.setattr(rows8, "library", lambda: lib)
-    monkeypatch.setattr(rows8.torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(rows8, "_current_device", lambda: 0)
     for m in (head, rows8):
         monkeypatch.setattr(m, "_stream", lambda stream, device: 0 if stream is None else stream.cuda_stream)
     return lib
