@@ -567,7 +567,7 @@ __global__ __launch_bounds__(1024) void k_gemm_rows(GemmArgs g)
 // B's rows within a pair of 16-row fragments are taken in the order
 // n = 8 (r / 4) + 4 t + r % 4 (fragment t, row r), which leaves each lane
 // eight neighbouring n of its row of A: one 16-byte store for 16-bit types.
-// Bound by memory: f16 409,600 x 256 to 64 58 us (4.5 TB/s); with A's rows
+// Bound by memory: f16 409,600 x 256 to 64 52 us (5.0 TB/s); with A's rows
 // loaded straight into fragments 72 us, sixteen lines to a quarter wave.
 // Chunk c of row n lies at c ^ swizzle(n), so that eight lanes' reads meet all
 // the banks in that order.
