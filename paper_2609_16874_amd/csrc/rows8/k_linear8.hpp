@@ -188,18 +188,18 @@ __device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float 
 // products that fill the chip with them.  What bounds the tiles is LDS: a step
 // reads and writes 96 KB for 128 x 128 outputs and 256 KB for 256 x 256, four times
 // as many (at 128 bytes a clock 2048 clocks, as long as the multiplies take).
-// Their sums leave from the registers, a lane's eight neighbours at a time, past
-// the caches, where the operands stay (16384 x 4096 to 4096 with SiLU 240 us, 262
-// through the caches, 242 through LDS); those of 128 x 128 tiles pass through LDS, so
+// Their sums leave from the registers, a lane's eight neighbours at a time, PAST
+// the caches where rows are whole lines, and the operands stay there (16384 x 4096 to
+// 4096 with SiLU 240 us, 262 through the caches, 242 through LDS); those of 128 x 128 tiles pass through LDS, so
 // that rows leave as whole lines (409,600 x 512 to 256 200 us, 212 from registers).
 //
 // Measured (one MI355X, bf16 out): 16384 x 4096 to 4096 with SiLU 223 us (2.5 POP/s),
 // with a residual, whose 134 MB arrive while nothing is multiplied, 262; 7744 x 1024
 // to 4096 with GELU 50; in 128 x 128 tiles 7744 x 4096 to 1024 41, 2048^3 19 us.
-template <bool WIDE, bool DIRECT, typename T, int ACT>
+template <bool WIDE, bool PAST, bool DIRECT, typename T, int ACT>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
 {
-    static_assert(DIRECT || !WIDE, "");
+    static_assert((DIRECT || !WIDE) && (WIDE || !PAST), "");
     constexpr int TM = WIDE ? 256 : 128, TN = TM, WM = 2, WN = WIDE ? 4 : 2, kThreads = WM * WN * 64;
     using A = ByteOperand<TM, kThreads, DIRECT>;
     using B = ByteOperand<TN, kThreads, DIRECT, WIDE>;
@@ -345,11 +345,11 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
                             const float y = activate<ACT>(z[v]);
                             o.v[v] = (T)(g.residual ? y + (float)r[i][p].v[v] : y);
                         }
-                        store_words<true>(out + 16 * (i0 + i) * g.ldo + 32 * p, o);
+                        store_words<PAST>(out + 16 * (i0 + i) * g.ldo + 32 * p, o);
                         if (g.preact) {
 #pragma unroll
                             for (int v = 0; v < 8; v++) o.v[v] = (T)z[v];
-                            store_words<true>(pre + 16 * (i0 + i) * g.ldp + 32 * p, o);
+                            store_words<PAST>(pre + 16 * (i0 + i) * g.ldp + 32 * p, o);
                         }
                     }
                 __builtin_amdgcn_sched_barrier(0);
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
                 const int m = m0 + wm + 16 * i + row;
                 const i32x4 v0 = acc[i][2 * p], v1 = acc[i][2 * p + 1];
                 const int32_t v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                if (m < g.m) finish8<ACT, true, T>(args, m, n, s[i], c, v);
+                if (m < g.m) finish8<ACT, PAST, T>(args, m, n, s[i], c, v);
             }
         }
         return;
@@ -604,6 +604,16 @@ inline bool wide8_pays(const GemmArgs &g)
     return 10 * others > 17 * wide;
 }
 
+// Whether rows of T are whole cache lines, so that wide tiles store past the
+// caches: halves of lines cost more there where they are not (38,884 x 1088 to 1264
+// with the value before the activation 162 us, 118 through the caches; to 1280 95
+// and 103), and in binary32 (142, 138).
+template <typename T>
+bool whole_lines8(const void *p, int64_t ld)
+{
+    return !p || (aligned_to(p, 128) && ld * (int64_t)sizeof(T) % 128 == 0);
+}
+
 template <typename T, int ACT>
 hipError_t launch_tiles8(Gemm8Args a, hipStream_t stream)
 {
@@ -616,12 +626,15 @@ hipError_t launch_tiles8(Gemm8Args a, hipStream_t stream)
     if (!wide) choose_splits8(a.g);
     const dim3 grid(a.g.tiles_m * a.g.tiles_n * a.g.splits);
     const int lds = 4 * tile * kStep8;
-    if (wide)
-        hipLaunchKernelGGL((k_gemm8<true, true, T, ACT>), grid, dim3(512), lds, stream, a);
+    constexpr bool kPast = sizeof(T) == 2;
+    if (wide && kPast && whole_lines8<T>(a.g.out, a.g.ldo) && whole_lines8<T>(a.g.preact, a.g.ldp))
+        hipLaunchKernelGGL((k_gemm8<true, kPast, true, T, ACT>), grid, dim3(512), lds, stream, a);
+    else if (wide)
+        hipLaunchKernelGGL((k_gemm8<true, false, true, T, ACT>), grid, dim3(512), lds, stream, a);
     else if (direct)
-        hipLaunchKernelGGL((k_gemm8<false, true, T, ACT>), grid, dim3(256), lds, stream, a);
+        hipLaunchKernelGGL((k_gemm8<false, false, true, T, ACT>), grid, dim3(256), lds, stream, a);
     else
-        hipLaunchKernelGGL((k_gemm8<false, false, T, ACT>), grid, dim3(256), lds, stream, a);
+        hipLaunchKernelGGL((k_gemm8<false, false, false, T, ACT>), grid, dim3(256), lds, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.g.splits == 1) return e;
     const int64_t quads = (int64_t)a.g.m * ((a.g.n + 3) / 4);
     hipLaunchKernelGGL((k_gemm8_join<T, ACT>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, stream, a);

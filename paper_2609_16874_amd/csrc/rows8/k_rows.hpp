@@ -423,7 +423,8 @@ __global__ __launch_bounds__(row_threads<LANES>(), grad_waves(LANES, N *V)) void
         }
     }
     if (!a.dgamma) return;
-    float *part = a.part + (int64_t)blockIdx.x * a.width;
+    // (one workgroup has all the sums: there is nothing to join)
+    float *part = a.blocks == 1 ? a.dgamma : a.part + (int64_t)blockIdx.x * a.width;
     if constexpr (R > 1) {
         // a wave's rows' sums first, by the lanes that have the same columns
         constexpr int kWaves = kRowThreads / 64;
@@ -562,6 +563,10 @@ hipError_t launch_pack_type(const RowsArgs &a, hipStream_t stream) { return laun
 template <typename T>
 hipError_t launch_rms_type(const RowsArgs &a, hipStream_t stream) { return launch_rows_type<T, true>(a, stream); }
 
+// Turns of one workgroup up to which the gradient is its alone, without the join's
+// launch.
+constexpr int alone_turns(int lanes) { return lanes <= 64 ? 8 : 1; }
+
 template <typename T>
 hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
 {
@@ -573,7 +578,7 @@ hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
         const int64_t most = rms_most_blocks(a.width);
         // (of no rows: one workgroup, whose partial sums are 0)
         const int64_t blocks = row_blocks<F::LANES>(a.rows > 0 ? a.rows : 1, grad_waves(F::LANES, F::N * F::V));
-        a.blocks = (int32_t)(blocks < most ? blocks : most);
+        a.blocks = (int32_t)(blocks <= alone_turns(F::LANES) ? 1 : blocks < most ? blocks : most);
         const dim3 grid(a.blocks), block(row_threads<F::LANES>());
         constexpr bool kPast = F::V * sizeof(T) == 16 && sizeof(T) == 2;
         auto launch = [&](auto packed, auto beyond) {
@@ -590,7 +595,7 @@ hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
             launch(std::false_type{}, std::false_type{});
         return hipGetLastError();
     });
-    if (e != hipSuccess || !a.dgamma) return e;
+    if (e != hipSuccess || !a.dgamma || a.blocks == 1) return e;
     hipLaunchKernelGGL(k_rms_join, dim3((unsigned)ceil_div(a.width, 32)), dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
