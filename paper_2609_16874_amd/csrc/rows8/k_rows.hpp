@@ -45,9 +45,11 @@ constexpr int rows_at_once() { return LANES <= 64 ? kRowThreads / LANES : 1; }
 // for them, and the grids fill the chip with them.
 constexpr int row_waves(int lanes, int elements) { return lanes > 256 ? 4 : elements <= 8 ? 6 : elements <= 16 ? 5 : 3; }
 constexpr int grad_waves(int lanes, int elements) { return lanes > 256 ? 4 : elements <= 8 ? 5 : elements <= 16 ? 3 : 2; }
-// Whether the next row's loads are in flight with the present one's work, and
-// gamma stays (the registers of the longest rows do not hold them).
-constexpr bool row_ahead(int lanes) { return lanes <= 256; }
+// Whether the next row's loads are in flight with the present one's work, and the
+// gradient's gamma stays: not where the registers do not hold them, nor in the norm
+// of longer rows, which writes as much as it reads (16,384 x 3000 in f32 packed 43 us
+// with them, 54 without; normed and added to a residual 121 and 114).
+constexpr bool row_ahead(int lanes, int elements, bool norm) { return lanes <= 256 || (elements <= 8 && !norm); }
 
 // op over the LANES threads of a row, in a fixed order, for all of them.
 // Steps 1, 2, 4 and 8 within rows of sixteen lanes by DPP (quads permuted, then
@@ -243,15 +245,16 @@ __global__ __launch_bounds__(row_threads<LANES>(), row_waves(LANES, N *V)) void 
         return raw;
     };
     int turn = 0;
+    constexpr bool AHEAD = row_ahead(LANES, N * V, NORM);
     const int64_t step = (int64_t)gridDim.x * R;
     int64_t base = (int64_t)blockIdx.x * R;
     [[maybe_unused]] Raw next;
-    if constexpr (row_ahead(LANES)) next = fetch(base);
+    if constexpr (AHEAD) next = fetch(base);
     [[maybe_unused]] float gamma[N][V];
     if constexpr (NORM) load_gamma<V, N>(a.gamma, share.at, gamma);
     for (; base < a.rows; base += step) {
-        const Raw raw = row_ahead(LANES) ? next : fetch(base);
-        if (row_ahead(LANES) && base + step < a.rows) next = fetch(base + step);
+        const Raw raw = AHEAD ? next : fetch(base);
+        if (AHEAD && base + step < a.rows) next = fetch(base + step);
         const int64_t row = base + group;
         const bool on = row < a.rows;
         float h[N][V];
@@ -373,25 +376,26 @@ __global__ __launch_bounds__(row_threads<LANES>(), grad_waves(LANES, N *V)) void
         return raw;
     };
     int turn = 0;
+    constexpr bool AHEAD = row_ahead(LANES, N * V, false);
     const int64_t step = (int64_t)gridDim.x * R;
     int64_t base = (int64_t)blockIdx.x * R;
     [[maybe_unused]] Raw next;
-    if (row_ahead(LANES) && base < a.rows) next = fetch(base);
+    if (AHEAD && base < a.rows) next = fetch(base);
     float gamma[N][V], acc[N][V];
-    if constexpr (row_ahead(LANES)) load_gamma<V, N>(a.gamma, share.at, gamma);
+    if constexpr (AHEAD) load_gamma<V, N>(a.gamma, share.at, gamma);
 #pragma unroll
     for (int i = 0; i < N; i++)
 #pragma unroll
         for (int v = 0; v < V; v++) acc[i][v] = 0.0f;
     for (; base < a.rows; base += step) {
-        Raw raw = row_ahead(LANES) ? next : fetch(base);
-        if (row_ahead(LANES) && base + step < a.rows) next = fetch(base + step);
+        Raw raw = AHEAD ? next : fetch(base);
+        if (AHEAD && base + step < a.rows) next = fetch(base + step);
         const int64_t row = base + group;
         const bool on = row < a.rows;
         if (base + R > a.rows && !on) {         // (a row that is not there adds nothing)
             raw = Raw{};
         }
-        if constexpr (!row_ahead(LANES)) load_gamma<V, N>(a.gamma, share.at, gamma);
+        if constexpr (!AHEAD) load_gamma<V, N>(a.gamma, share.at, gamma);
         const float to_xh = PACKED ? raw.scale * raw.rstd : raw.rstd;
         float xh[N][V], t[N][V], sum = 0.0f;
 #pragma unroll
@@ -489,8 +493,13 @@ struct RowForm {
 };
 
 // call(form) for the first of these whose lanes hold the row; WIDEST: the
-// vectors that a row may have.
-template <typename T, int WIDEST, typename Call>
+// vectors that a row may have.  GRAD: one vector a thread where a row takes several
+// waves, so that the registers hold the next row's loads as well (4628 x 7488 in
+// bf16 42 us, 70 with two and no load ahead; 20,000 x 2048 in f32 with the gradient
+// past the norm 98 and 109; the other way round for packed rows of 5000 in f16, 8192 of
+// them 86 and 79).  The forward is slower so (8192 x 5000 in f16 to bytes 48 us, 37
+// with two).
+template <typename T, int WIDEST, bool GRAD, typename Call>
 hipError_t with_row_form(int width, Call call)
 {
     constexpr int V = kRowVec<T>;
@@ -502,6 +511,10 @@ hipError_t with_row_form(int width, Call call)
     if (vectors <= 64) return call(RowForm<V, 32, 2>{});
     if (vectors <= 128) return call(RowForm<V, 64, 2>{});
     if (vectors <= 256) return call(RowForm<V, 256, 1>{});
+    if constexpr (GRAD) {
+        if (vectors <= 512) return call(RowForm<V, 512, 1>{});
+        if (vectors <= 1024) return call(RowForm<V, 1024, 1>{});
+    }
     if (vectors <= 512) return call(RowForm<V, 256, 2>{});
     if (vectors <= 1024) return call(RowForm<V, 512, 2>{});
     if (vectors <= 2048) return call(RowForm<V, 1024, 2>{});
@@ -545,7 +558,7 @@ hipError_t launch_rows_type(RowsArgs a, hipStream_t stream)
                       goes_past<T>(a.rows, a.width, (1 + !!a.residual + !!a.sum + !!a.y) * (int)sizeof(T) + !!a.q) &&
                       whole_lines<T>(a.sum, a.lds) && whole_lines<T>(a.y, a.ldy);
     constexpr int kWidest = NORM ? kRmsMaxChannels : kRowsMaxWidth;
-    return with_row_form<T, kWidest / kRowVec<T>>(a.width, [&](auto form) {
+    return with_row_form<T, kWidest / kRowVec<T>, false>(a.width, [&](auto form) {
         using F = decltype(form);
         const dim3 grid((unsigned)row_blocks<F::LANES>(a.rows, row_waves(F::LANES, F::N * F::V)));
         constexpr bool kPast = NORM && F::V * sizeof(T) == 16 && sizeof(T) == 2;
@@ -574,7 +587,7 @@ hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
     a.inverse_width = 1.0f / (float)a.width;
     const bool past = a.dx && whole_lines<T>(a.dx, a.ldx) &&
                       goes_past<T>(a.rows, a.width, (2 + !!a.dsum) * (int)sizeof(T) + (a.h_scale ? 1 : (int)sizeof(T)));
-    const hipError_t e = with_row_form<T, kRmsMaxChannels / kRowVec<T>>(a.width, [&](auto form) {
+    const hipError_t e = with_row_form<T, kRmsMaxChannels / kRowVec<T>, true>(a.width, [&](auto form) {
         using F = decltype(form);
         const int64_t most = rms_most_blocks(a.width);
         // (of no rows: one workgroup, whose partial sums are 0)
