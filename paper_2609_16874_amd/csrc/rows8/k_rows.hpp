@@ -514,9 +514,10 @@ hipError_t with_row_form(int width, Call call)
     if constexpr (GRAD) {
         if (vectors <= 512) return call(RowForm<V, 512, 1>{});
         if (vectors <= 1024) return call(RowForm<V, 1024, 1>{});
+    } else {
+        if (vectors <= 512) return call(RowForm<V, 256, 2>{});
+        if (vectors <= 1024) return call(RowForm<V, 512, 2>{});
     }
-    if (vectors <= 512) return call(RowForm<V, 256, 2>{});
-    if (vectors <= 1024) return call(RowForm<V, 512, 2>{});
     if (vectors <= 2048) return call(RowForm<V, 1024, 2>{});
     if constexpr (WIDEST > 2048)
         if (vectors <= 4096) return call(RowForm<V, 1024, 4>{});

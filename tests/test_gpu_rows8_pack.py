@@ -17,6 +17,7 @@ SHAPES = [
     (17, 100, 0, 0), (1000, 127, 0, 0), (129, 256, 8, 0), (64, 511, 0, 0), (3000, 512, 0, 0), (10, 1001, 3, 2),
     (2, 2049, 0, 0), (65, 4096, 0, 0), (3, 4104, 0, 1), (4, 8191, 0, 0), (5, 10000, 24, 0), (2, 16384, 0, 0), (3, 16391, 0, 0),
     (2, 40001, 0, 0), (1, 65536, 0, 0), (70001, 24, 0, 0), (30000, 260, 4, 0),
+    (1500, 2500, 0, 0), (900, 4100, 8, 0), (700, 7000, 0, 1), (600, 9000, 0, 0),    # (several turns of a workgroup per row)
 ]
 
 
