@@ -87,6 +87,28 @@ def test_ties_go_to_the_even_number():
     assert q.cpu().tolist() == [[127, 0, 2, 2, 0, -2, 3, 4, 126]]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quotients_of_the_smallest_rows(dtype):
+    """Rows whose largest value is 2^-126 to 2^-95, with values in the middle of
+    two bytes and next to it: x - q s is then as small as binary32's smallest
+    numbers, and the bytes are still those of a division (rounded once, ties of
+    rint to even)."""
+    M, C = 4000, 61
+    g = torch.Generator().manual_seed(11)
+    largest = torch.exp2(torch.randint(-126, -95, (M, 1), generator=g).float()) * (1.0 + torch.rand((M, 1), generator=g))
+    largest = largest.to(DTYPES[dtype]).float()
+    scale = (largest / 127.0).clamp(min=LEAST)
+    x = scale * (torch.randint(0, 127, (M, C), generator=g).float() + 0.5)
+    x = (x.view(torch.int32) + torch.randint(-1, 2, (M, C), generator=g, dtype=torch.int32)).view(torch.float32)
+    x = torch.minimum(x, largest) * (2.0 * torch.randint(0, 2, (M, C), generator=g) - 1.0)
+    x[:, :1] = largest
+    x = x.to(DTYPES[dtype])
+    x[:, 1:] = torch.where(x[:, 1:].abs() > x[:, :1], x[:, :1], x[:, 1:])      # (a rounding to bf16 may pass it)
+    q, got = rows8().packed(x.cuda())
+    assert torch.equal(got.cpu(), scale[:, 0])
+    assert torch.equal(q.cpu(), torch.round(x.float() / scale).to(torch.int8))
+
+
 def test_a_second_packing_changes_nothing():
     """The values of rows in 8 bits, packed again, are the same rows (their
     largest is 127 s to a rounding)."""
