@@ -12,6 +12,7 @@ from __future__ import annotations
 import torch
 
 from . import head, native, rows8
+from .head import _unrecorded
 
 
 class PixelBlock:
@@ -38,8 +39,10 @@ class PixelBlock:
 
     def forward(self, x, residual=None):
         """(y, sum) of x [rows][channels] and the stream before it (none: x
-        begins it); keeps what ``backward`` needs."""
+        begins it); keeps what ``backward`` needs.  Not recorded by autograd:
+        tensors that require a gradient are refused while it records."""
         p = self.params
+        _unrecorded("PixelBlock.forward", x, residual, p["gamma"])
         total = x if residual is None else torch.empty_like(x)
         u = torch.empty_like(x)
         rstd = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)

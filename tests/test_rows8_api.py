@@ -265,3 +265,15 @@ def test_outputs_are_allocated_on_the_stream_that_writes_them(given, recorded, m
     _linear8().run(q, s, Tensor((6, 8), I8), Tensor((6,), F32), keep=True, stream=stream)
     _linear().run_backward8(q, s, Tensor((6, 8)), y, Tensor((4, 6), I8), s, stream=stream)
     assert len(inside) == 14 and all(t is stream for t in inside)
+
+
+@pytest.mark.parametrize("which", ["x", "residual", "gamma"])
+def test_a_block_that_would_lose_a_gradient_refuses(which):
+    """(The norm writes into tensors of the block's own, which no autograd sees.)"""
+    from paper_2609_16874_amd.pixel_block import PixelBlock
+    t = {k: torch.zeros((4, 8) if k != "gamma" else 8, requires_grad=k == which) for k in ("x", "residual", "gamma")}
+    b = object.__new__(PixelBlock)
+    b.params, b.checkpoint8, b.norm = {"gamma": t["gamma"]}, False, _rms()
+    with pytest.raises(ValueError, match="autograd"):
+        b.forward(t["x"], t["residual"])
+    assert b.norm._lib.calls == []
