@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 #include <type_traits>
 
 #include "cpe_head.h"
@@ -144,6 +145,13 @@ __device__ __forceinline__ int xcd_order(int w, int n)
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+// Whether an output (null: not wanted) is none of these arguments of its call.
+inline bool apart(const void *out, std::initializer_list<const void *> others)
+{
+    for (const void *p : others)
+        if (out && out == p) return false;
+    return true;
+}
 inline size_t element_size(cpe_head_dtype t) { return t == CPE_HEAD_F32 ? 4 : 2; }
 inline size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 

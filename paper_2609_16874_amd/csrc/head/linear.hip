@@ -142,8 +142,10 @@ cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, con
         if (dx && (!check_matrix(h, w, w_ld, h->in) || !check_matrix(h, dx, dx_ld, h->in)))
             return CPE_ERR_INVALID_ARG;
         if (dw && !check_kept(x, h->in)) return CPE_ERR_INVALID_ARG;
-        if (dx && (dx == dy || dx == x.p || dx == w || dx == preact.p)) return CPE_ERR_INVALID_ARG;
-        if (dw && (dw == dy || dw == x.p || dw == w || dw == preact.p || dw == dx)) return CPE_ERR_INVALID_ARG;
+        if (!apart(dx, {dy, x.p, x.scale, w, preact.p, preact.scale}) ||
+            !apart(dw, {dy, x.p, x.scale, w, preact.p, preact.scale, dx}) ||
+            !apart(dbias, {dy, x.p, x.scale, w, preact.p, preact.scale, dx, dw}))
+            return CPE_ERR_INVALID_ARG;
     }
     if (dw && !check_matrix(h, dw, dw_ld, h->in)) return CPE_ERR_INVALID_ARG;
     (void)hipGetLastError();

@@ -79,11 +79,11 @@ cpe_status cpe_linear8_forward(cpe_linear8 *h, hipStream_t stream, int32_t rows,
     if (!check_matrix(q, q_ld, h->in, 1) || !check_matrix(w, w_ld, h->in, 1) || !scale || !w_scale ||
         !check_matrix(y, y_ld, h->out, element))
         return CPE_ERR_INVALID_ARG;
-    if (y == q || y == w) return CPE_ERR_INVALID_ARG;       // (other workgroups still read them)
+    if (!apart(y, {q, scale, w, w_scale, bias})) return CPE_ERR_INVALID_ARG;     // (other workgroups still read them)
     if (residual && !check_matrix(residual, residual_ld, h->out, element)) return CPE_ERR_INVALID_ARG;
     if (residual == y && residual_ld != y_ld) return CPE_ERR_INVALID_ARG;
-    if (preact && (!check_matrix(preact, preact_ld, h->out, element) || preact == y || preact == residual ||
-                   preact == q || preact == w))
+    if (preact && (!check_matrix(preact, preact_ld, h->out, element) ||
+                   !apart(preact, {q, scale, w, w_scale, bias, residual, y})))
         return CPE_ERR_INVALID_ARG;
     Gemm8Args a{};
     a.a_scale = scale;

@@ -60,7 +60,7 @@ cpe_status cpe_rows8_pack(hipStream_t stream, int32_t rows, int32_t width, cpe_h
         return CPE_ERR_INVALID_ARG;
     if (rows == 0) return CPE_OK;
     if (!check_rows(x, x_ld, width, element_size(dtype)) || !check_rows(q, q_ld, width, 1) || !scale ||
-        !aligned_to(scale, 4) || q == x || (const void *)scale == x || (void *)scale == (void *)q)
+        !aligned_to(scale, 4) || !apart(q, {x}) || !apart(scale, {x, q}))
         return CPE_ERR_INVALID_ARG;
     RowsArgs a{};
     a.x = x;
@@ -80,7 +80,7 @@ cpe_status cpe_rows8_unpack(hipStream_t stream, int32_t rows, int32_t width, con
         return CPE_ERR_INVALID_ARG;
     if (rows == 0) return CPE_OK;
     if (!check_rows(x, x_ld, width, element_size(dtype)) || !check_rows(q, q_ld, width, 1) || !scale ||
-        !aligned_to(scale, 4) || x == q || x == scale)
+        !aligned_to(scale, 4) || !apart(x, {q, scale}))
         return CPE_ERR_INVALID_ARG;
     UnpackArgs a{};
     a.q = q;
@@ -140,10 +140,11 @@ cpe_status cpe_rms_forward(cpe_rms *h, hipStream_t stream, int32_t rows, const v
                 !in_place(sum, sum_ld, residual, residual_ld)))
         return CPE_ERR_INVALID_ARG;
     if (y && (!check_rows(y, y_ld, C, element) || !in_place(y, y_ld, x, x_ld) ||
-              !in_place(y, y_ld, residual, residual_ld) || y == sum))
+              !in_place(y, y_ld, residual, residual_ld)))
         return CPE_ERR_INVALID_ARG;
-    if (!q != !scale || (scale && scale == rstd)) return CPE_ERR_INVALID_ARG;
-    if (q && (!check_rows(q, q_ld, C, 1) || q == x || q == residual || q == sum || q == y))
+    if (!q != !scale || (q && !check_rows(q, q_ld, C, 1))) return CPE_ERR_INVALID_ARG;
+    if (!apart(sum, {gamma}) || !apart(y, {gamma, sum}) || !apart(q, {x, residual, gamma, sum, y}) ||
+        !apart(scale, {x, residual, gamma, sum, y, q}) || !apart(rstd, {x, residual, gamma, sum, y, q, scale}))
         return CPE_ERR_INVALID_ARG;
     RowsArgs a{};
     a.x = x;
@@ -182,6 +183,8 @@ cpe_status cpe_rms_backward(cpe_rms *h, hipStream_t stream, int32_t rows, const 
         if (dsum && !check_rows(dsum, dsum_ld, C, element)) return CPE_ERR_INVALID_ARG;
         if (dx && (!check_rows(dx, dx_ld, C, element) || !in_place(dx, dx_ld, dy, dy_ld) ||
                    !in_place(dx, dx_ld, dsum, dsum_ld) || (dx == h_rows && (h_scale || dx_ld != h_ld))))
+            return CPE_ERR_INVALID_ARG;
+        if (!apart(dx, {h_scale, gamma, rstd}) || !apart(dgamma, {h_rows, h_scale, dy, gamma, rstd, dsum, dx}))
             return CPE_ERR_INVALID_ARG;
     } else if (!dgamma) {
         return CPE_OK;
