@@ -594,11 +594,6 @@ hipError_t launch_pack_type(const RowsArgs &a, hipStream_t stream) { return laun
 template <typename T>
 hipError_t launch_rms_type(const RowsArgs &a, hipStream_t stream) { return launch_rows_type<T, true>(a, stream); }
 
-// Turns of one workgroup up to which the gradient is its alone, without the join's
-// launch: a call on 16 x 1024 in bf16 takes 6.5 us, on 32 x 1024 9.0, with the join 9.8;
-// of a row in more than a wave 4 x 8192 10.0 against 9.8.
-constexpr int alone_turns(int lanes) { return lanes <= 64 ? 8 : 1; }
-
 template <typename T>
 hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
 {
@@ -607,10 +602,9 @@ hipError_t launch_rms_grad_type(RmsGradArgs a, hipStream_t stream)
                       goes_past<T>(a.rows, a.width, (2 + !!a.dsum) * (int)sizeof(T) + (a.h_scale ? 1 : (int)sizeof(T)));
     const hipError_t e = with_row_form<T, kRmsMaxChannels / kRowVec<T>, true>(a.width, [&](auto form) {
         using F = decltype(form);
-        const int64_t most = rms_most_blocks(a.width);
         // (of no rows: one workgroup, whose partial sums are 0)
-        const int64_t blocks = row_blocks<F::LANES>(a.rows > 0 ? a.rows : 1, grad_waves(F::LANES, F::N * F::V));
-        a.blocks = (int32_t)(blocks <= alone_turns(F::LANES) ? 1 : blocks < most ? blocks : most);
+        const int64_t want = row_blocks<F::LANES>(a.rows > 0 ? a.rows : 1, grad_waves(F::LANES, F::N * F::V));
+        a.blocks = rms_grad_blocks(want, a.width, F::LANES, a.dgamma != nullptr);
         const dim3 grid(a.blocks), block(row_threads<F::LANES>());
         constexpr bool kPast = F::V * sizeof(T) == 16 && sizeof(T) == 2;
         auto launch = [&](auto packed, auto beyond) {

@@ -23,6 +23,17 @@ inline int rms_most_blocks(int32_t channels)
     return by_bytes > kRmsMaxBlocks ? kRmsMaxBlocks : by_bytes < 256 ? 256 : by_bytes;
 }
 
+// Workgroups of a gradient whose rows fill `want` of them: `lanes` threads take a
+// row.  Up to eight turns of one workgroup of several rows at once are its alone,
+// without the launch that joins dgamma: a call on 16 x 1024 in bf16 takes 6.4 us, on
+// 32 x 1024 8.9, with the join 9.2; of a row in more than a wave 4 x 8192 10.0 against
+// 9.2.  Without dgamma there is no join: 32 x 1024 in one workgroup 8.4, in eight 6.4.
+inline int32_t rms_grad_blocks(int64_t want, int32_t channels, int lanes, bool dgamma)
+{
+    const int64_t most = rms_most_blocks(channels), alone = lanes <= 64 ? 8 : 1;
+    return (int32_t)(dgamma && want <= alone ? 1 : want < most ? want : most);
+}
+
 // h = x (+ residual, rounded), y = h rstd gamma (norm), or y = x; any of
 // h, y, y packed and rstd.
 struct RowsArgs {
