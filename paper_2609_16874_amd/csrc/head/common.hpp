@@ -23,7 +23,9 @@ struct __attribute__((packed, aligned(sizeof(T)))) Vec {
 
 // (Stored as one vector of words: from the structure the compiler makes pieces of
 // three words, one and a half where the same code stores single elements too, and
-// the stores of 16-bit rows reach two thirds of their rate.)  PAST: past the caches.
+// the stores of 16-bit rows reach two thirds of their rate.  The group norm's gradient
+// of 307,039 x 100 in f16 with ReLU takes 40 registers more so, which leaves three
+// waves of a SIMD instead of four, and 70 us instead of 74.)  PAST: past the caches.
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
 {

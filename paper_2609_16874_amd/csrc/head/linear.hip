@@ -210,8 +210,10 @@ cpe_status backward(cpe_linear *h, hipStream_t stream, int32_t rows, Kept x, con
     }
     // With many n x in 8 bits becomes x of the dtype in the place of dx, which is
     // written after dw then: dw's tiles would convert each byte once for every 128 n
-    // (7744 x 1024 to 4096 219 us in all, 225 otherwise; 7744 x 4096 to 1024 186 and
-    // 189; 50,000 x 512 to 512 151 and 133).
+    // (bf16 with GELU: 7744 x 1024 to 4096 189 us in all, 204 otherwise; to 2048 116
+    // and 123; to 1024 85 and 84).  Many rows of few features pay for the unpacking
+    // (50,000 x 512 to 2048 425 and 405, to 512 163 and 137), those of more gain below
+    // the threshold as well (7744 x 4096 to 1536 254 and 282).
     const bool first_dw = dw && dx && rows > 0 && x.scale && h->out >= 2048;
     auto run_dx = [&]() {       // dx[r][k] = sum_n dz[r][n] w[n][k]
         GemmArgs g{};

@@ -182,7 +182,7 @@ __device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float 
 // alternate in registers, the waves meet once a step, and at the meeting the
 // next step's LDS tile has arrived.  A half's LDS reads (and the next tile's
 // loads) are spread over its multiplies: left to itself the compiler puts them
-// last, and the waves wait for them (16384 x 4096 to 4096 302 us, spread 285).
+// last, and the waves wait for them (6 % of 16384 x 4096 to 4096).
 //
 // WIDE: tiles of 256 x 256 and waves of 128 x 64, one workgroup per CU, for
 // products that fill the chip with them.  What bounds the tiles is LDS: a step
@@ -190,12 +190,14 @@ __device__ __forceinline__ void finish8(const Gemm8Args &a, int m, int n, float 
 // as many (at 128 bytes a clock 2048 clocks, as long as the multiplies take).
 // Their sums leave from the registers, a lane's eight neighbours at a time, PAST
 // the caches where rows are whole lines, and the operands stay there (16384 x 4096 to
-// 4096 with SiLU 240 us, 262 through the caches, 242 through LDS); those of 128 x 128 tiles pass through LDS, so
-// that rows leave as whole lines (409,600 x 512 to 256 200 us, 212 from registers).
+// 4096 with SiLU 222 us, 233 through the caches); those of 128 x 128 tiles pass
+// through LDS, so that rows leave as whole lines (straight from registers 409,600 x
+// 512 to 256 took 6 % longer in such tiles).
 //
-// Measured (one MI355X, bf16 out): 16384 x 4096 to 4096 with SiLU 223 us (2.5 POP/s),
-// with a residual, whose 134 MB arrive while nothing is multiplied, 262; 7744 x 1024
-// to 4096 with GELU 50; in 128 x 128 tiles 7744 x 4096 to 1024 41, 2048^3 19 us.
+// Measured (one MI355X, bf16 out, other data from call to call): 16384 x 4096 to 4096
+// with SiLU 222 us (2.5 POP/s), with a residual, whose 134 MB arrive while nothing is
+// multiplied, 262; 7744 x 1024 to 4096 with GELU 50; 409,600 x 512 to 256 in f16 121
+// to 131; in 128 x 128 tiles 7744 x 4096 to 1024 38, 2048^3 18 us.
 template <bool WIDE, bool PAST, bool DIRECT, typename T, int ACT>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
 {
@@ -315,8 +317,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
         }
         if (m0 + TM <= g.m && n0 + TN <= g.n) {
             // A whole tile: both halves of a line follow one another, and the
-            // residual's loads of two rows are in flight together (16384 x 4096 to
-            // 4096 276 us; the halves apart 290, one load at a time 308).
+            // residual's loads of two rows are in flight together (the halves apart
+            // cost 16384 x 4096 to 4096 5 %, one load at a time 12 %).
             static_assert(FN == 4 || !WIDE, "");
             constexpr int kBatch = 2;
             const T *res = static_cast<const T *>(g.residual) + (m0 + wm + row) * g.ldr + n0 + wn + 8 * group;
@@ -400,9 +402,10 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_gemm8(Gemm8Args args)
 // Narrow products (a map's projection to its embedding), whose B fits into LDS
 // whole, as those of 16 bits: B is laid out once per workgroup, strips of 64 rows
 // of A stream past it, each read once, in whole lines, with the next strip's loads
-// in flight.  Bound by memory: 409,600 x 256 to 64 in f16 31 us (5.1 TB/s) with four
-// workgroups per CU; three 33, strips of 128 rows 33 to 36 (a round of them more or
-// less is then a sixth of the work).
+// in flight.  Bound by memory: 409,600 x 256 to 64 in f16 38 us (4.1 TB/s; in tiles
+// 72).  On the same rows again and again, which the last cache holds in part, 30 with
+// four workgroups per CU; three 33, strips of 128 rows 33 to 36 (a round of them more
+// or less is then a sixth of the work).
 constexpr int kStrip8 = 64;
 constexpr int narrow8_bytes(int n, int ks) { return ((n + 31) / 32 * 32 + kStrip8) * ks * 64; }
 
@@ -594,9 +597,10 @@ inline void choose_splits8(GemmArgs &g)
 }
 
 // Rounds of tiles that the chip goes through: a round of wide ones (256 at
-// once) takes 1.4 to 1.85 times as long as one of the others (512 at once):
-// 7744 x 4096 to 1024 59 against 42 us, a round each; 4096^3 71 against 83, one
-// against two; 7744 x 1024 to 4096 67 against 72, two against four.
+// once) takes 1.15 to 1.7 times as long as one of the others (512 at once):
+// 7744 x 4096 to 1024 42 against 37 us, a round each; 4096^3 57 against 71, one
+// against two; 7744 x 1024 to 4096 40 against 51, two against four; 409,600 x 512 to
+// 256 in f16 121 against 170, seven against thirteen.
 inline bool wide8_pays(const GemmArgs &g)
 {
     const int64_t wide = ceil_div(ceil_div(g.m, 256) * ceil_div(g.n, 256), 256);
@@ -606,8 +610,8 @@ inline bool wide8_pays(const GemmArgs &g)
 
 // Whether rows of T are whole cache lines, so that wide tiles store past the
 // caches: halves of lines cost more there where they are not (38,884 x 1088 to 1264
-// with the value before the activation 162 us, 118 through the caches; to 1280 95
-// and 103), and in binary32 (142, 138).
+// with the value before the activation 155 us, 113 through the caches; to 1280 91
+// and 103, without that value 68 and 77), and in binary32 (169, 131).
 template <typename T>
 bool whole_lines8(const void *p, int64_t ld)
 {
@@ -643,8 +647,8 @@ hipError_t launch_tiles8(Gemm8Args a, hipStream_t stream)
 
 // Fragments of k that hold a row (2, 4 or 8), 0 where it is too long.
 inline int narrow8_steps(int k) { return k <= 128 ? 2 : k <= 256 ? 4 : k <= 512 ? 8 : 0; }
-// Where two workgroups or more fit a CU: 409,600 x 512 to 96 70 us (in tiles 85),
-// to 128, of which one fits, 122 (92).
+// Where two workgroups or more fit a CU: 409,600 x 512 to 96 in f16 74 us (in tiles
+// 95), to 128, of which one fits, 124 (100).
 inline bool narrow8_fits(const GemmArgs &g)
 {
     const int ks = narrow8_steps(g.k);

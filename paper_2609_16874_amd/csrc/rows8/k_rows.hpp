@@ -4,7 +4,9 @@
 //
 // A row belongs to LANES neighbouring threads, N vectors of V elements each,
 // and stays in their registers between its reduction and what is written: each
-// input is read once.  Up to 64 lanes a row's sums pass between the lanes of
+// input is read once.  (The widest forms spill some: packing more than 32,768 elements
+// 80 bytes a lane in f16, 20 in bf16, 12 in f32; the gradient of more than 8192
+// channels 28 to 36 in f32, 12 in 16 bits from packed rows.)  Up to 64 lanes a row's sums pass between the lanes of
 // its wave, beyond that through LDS.  Workgroups take rows in turn, with the
 // next row's loads in flight while the present one is worked on; gamma stays
 // in registers.
@@ -16,14 +18,16 @@
 // enough: what a row costs whatever its length (the steps of its reductions, its
 // root and quotients, about 80 instructions a wave) is shared by twice the elements
 // of one vector.  A root and two divisions of the compiler's would double it; the
-// hardware's approximations, corrected once, take their place.
+// hardware's approximations take their place, the quotients' corrected once, the
+// reciprocal root's (off by 2^-23 of it at most) as it is.
 //
-// Bound by memory.  Measured (one MI355X): 409,600 x 256 in f16 packed 59 us (5.4
-// TB/s), unpacked 52 (6.0), norm to y, bytes and rstd 97 (5.4; 137 with eight
-// elements a thread and the compiler's divisions); 7744 x 1024 in bf16 with the
-// residual, its sum and bytes 11 us (5.0); the gradient of 307,039 x 100 in f32 75 us
-// (4.9) and 4 for the join of dgamma; 4096 x 16384 in f16, a workgroup of 1024 threads
-// to a row and no load ahead, 90 (4.5).
+// Bound by memory.  Measured (one MI355X, other data from call to call): 409,600 x 256
+// in f16 packed 59 us (5.4 TB/s), unpacked right after 52 (6.0; 60 where the last cache
+// does not have the bytes; in f32 138, 3.8 TB/s), norm to y, bytes and rstd 97 (5.4;
+// 137 with eight elements a thread and the compiler's divisions); 7744 x 1024 in bf16
+// with the residual, its sum and bytes 11 us (5.0); the gradient of 307,039 x 100 in f32
+// 75 us (4.9) and 4 for the join of dgamma; 4096 x 16384 in f16, a workgroup of 1024
+// threads to a row and no load ahead, 90 (4.5).
 #pragma once
 
 #include "head/common.hpp"
@@ -512,10 +516,11 @@ struct RowForm {
 // call(form) for the first of these whose lanes hold the row; WIDEST: the
 // vectors that a row may have.  GRAD: one vector a thread where a row takes several
 // waves, so that the registers hold the next row's loads as well (4628 x 7488 in
-// bf16 42 us, 70 with two and no load ahead; 20,000 x 2048 in f32 with the gradient
-// past the norm 98 and 109; the other way round for packed rows of 5000 in f16, 8192 of
-// them 86 and 79).  The forward is slower so (8192 x 5000 in f16 to bytes 48 us, 37
-// with two).
+// bf16 46 us, 73 with two and no load ahead; 8192 x 5000 in f16 51 and 68; 20,000 x
+// 2048 in f32 95 and 98).  From packed rows it goes either way: 4628 x 7488 in bf16 55
+// and 70, 20,000 x 2048 in f32 with the gradient past the norm 98 and 108, but 8192 x
+// 5000 in f16 69 and 62, 16,384 x 2500 in bf16 72 and 61.  The forward is slower so
+// (8192 x 5000 in f16 to bytes 60 us, 37 with two).
 template <typename T, int WIDEST, bool GRAD, typename Call>
 hipError_t with_row_form(int width, Call call)
 {
@@ -547,10 +552,11 @@ hipError_t with_row_form(int width, Call call)
 
 // Whether what a call writes goes past the caches: where its rows, `bytes` for
 // each element, are more than the last cache holds, and the written ones are
-// whole lines of 16-bit values (409,600 x 256 in f16: unpacking 50 us against 64,
-// norm with y, q and rstd 98 against 101; 30,000 x 2048, which fits, norm 42
-// against 38; f32 unpacked in two stores a thread, half a line each, 55 against
-// 28).  Bytes stay in the caches, for the product that reads them next.
+// whole lines of 16-bit values (409,600 x 256 in f16: unpacking right after packing
+// 50 us against 64, norm with y, q and rstd 97 against 100; 30,000 x 2048, which fits,
+// norm 44 against 45 where nothing reads y, which would then find it in memory; f32
+// unpacked in two stores a thread, half a line each, 55 against 28).  Bytes stay in
+// the caches, for the product that reads them next.
 constexpr int64_t kCacheBytes = (int64_t)256 << 20;
 template <typename T>
 bool goes_past(int64_t rows, int64_t width, int64_t bytes)

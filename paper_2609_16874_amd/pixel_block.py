@@ -4,8 +4,10 @@ the residual stream's addition, a product with an activation, a product back.
 A block takes the last one's output and the stream before it, (x, residual), and
 returns its own output and the stream, (y, sum): the next norm adds the two, so
 the stream is read and written once a block.  ``PixelBlock`` trains, with its
-activations kept for the gradient as they are or in 8 bits (``checkpoint8``,
-half the memory or a quarter); ``PixelBlock8`` serves a trained one in integers.
+activations kept for the gradient as they are or in 8 bits (``checkpoint8``: half
+the memory or a quarter from a block's forward to its backward; while the forward
+runs its own activations are there as they are, too); ``PixelBlock8`` serves a
+trained one in integers.
 """
 from __future__ import annotations
 
